@@ -409,11 +409,92 @@ int q4_traceback(const q4_beam_state* state, int32_t B, int32_t W, int32_t n_ite
 int q4_feature_prologue(const float* mel, int32_t B, int32_t T100, int32_t M, void* out_fp16,
                         q4_stream stream);
 
+/* ---------------------------------------------------------------------------------------------------------------------
+ * Around the output of a language model: per-token 8-bit activations, and a label-synchronous beam search over whole
+ * vocabularies.  The paper's language models quantize with one boundary per tensor; the calls below give every token (row)
+ * its own MAX boundary (Section 3.1, "MAX"), which is what networks with normalised residual streams need.
+ *
+ * Element types of real-valued tensors in these calls.  Their rows may lie further apart than they are long (strides in
+ * elements), and x, residual, sum_out, out and logits need to be aligned to their elements only. */
+#define Q4_F32 0
+#define Q4_F16 1
+#define Q4_BF16 2
+
+/*
+ * q4_rmsnorm_quantize — root-mean-square norm of every row, written as 8-bit codes with one scale per row; with a residual
+ * its addition in front.  For each of `rows` rows of k values:
+ *   h = x, or x + residual rounded to dtype (and stored in sum_out; the norm is taken of the value as stored);
+ *   y_i = h_i * gain_i / sqrt(mean(h^2) + eps);
+ *   MAX boundary alpha = max |y_i| (1 for a row of zeros), scale_out = alpha / 127, code_i = y_i / scale_out rounded to the
+ *   nearest integer, halves to even.  The root is a common factor of the row: codes are those of
+ *   127 h_i gain_i / max |h gain|, decided in double where fp32 cannot tell, so they do not depend on the order of the sum.
+ * A row that holds a NaN or an infinity gets codes 0 and a NaN scale.  Values of any finite magnitude are accepted.
+ *   x [rows, k] dtype, row stride x_stride; residual (nullable) and sum_out (required with residual, refused without)
+ *   likewise; sum_out may be x or residual itself (same pointer and stride).  gain [k] fp32.  0 <= eps, finite.
+ *   q_out [rows, k_pad] codes as for quantize_pack_int4 (k_pad a multiple of 32, elements behind k are 0); scale_out [rows].
+ * Input of q4_linear_token_scales.  Counts as one activation quantizer (q4_quantizer_calls).
+ */
+int q4_rmsnorm_quantize(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, int32_t dtype,
+                        int64_t rows, int32_t k, int32_t k_pad, const float* gain, float eps, void* sum_out,
+                        int64_t sum_stride, void* q_out, float* scale_out, q4_stream stream);
+
+/*
+ * q4_linear_token_scales — quantized linear layer with a scale for every token:
+ * out[m, j] = acc[m, j] * (x_scale[m] * w.scale[j]) + bias[j], acc the exact int32 sum over k, the rest fp32, rounded once
+ * to out_dtype.
+ *   xq [M, w.k_pad] 8-bit codes (of q4_rmsnorm_quantize, or of quantize_pack_int4 in mode 1 with one group per row),
+ *   x_scale [M] fp32; w: 8-bit codes, k_pad at most 131040 (the sums stay below 2^31), its rows are the tensor cores'
+ *   operand as they are; bias (nullable) [w.rows]; out [M, w.rows] out_dtype, row stride out_stride.
+ *   status (nullable, device int32): receives Q4_ERR_TIMEOUT when a bounded device wait runs out (see q4_poll_status); it is
+ *   not written otherwise, so clear it once before the first call.
+ */
+int q4_linear_token_scales(const void* xq, const float* x_scale, int32_t M, const q4_mat* w, const float* bias, void* out,
+                           int32_t out_dtype, int64_t out_stride, int32_t* status, q4_stream stream);
+
+/*
+ * q4_lm_beam_select — one step of a label-synchronous beam search over beams and vocabulary, for B utterances of W beams:
+ *   log P(k) = z_k - log sum exp z of a beam's row of logits; beam w proposes every label k with
+ *   score[w] + log P(k) + rho (rho: the label bonus of Eq. 1); a beam that has ended (done != 0) proposes itself once, with
+ *   label eos and its score unchanged, and its logits are not looked at; the W best proposals are the next beams: score
+ *   descending, equal ones by parent, those of one beam by logit and then by label.
+ *   logits [B W, V] dtype, row stride logits_stride (>= V); score [B, W] fp32: a beam whose score is not finite is empty;
+ *   done (nullable) [B, W] bytes; eos: label that ends a hypothesis, -1 for none (then done must be NULL).
+ *   parent, token [B, W]: beam the proposal came from and its label, -1 where there are fewer than W proposals;
+ *   score_out [B, W]: its score (-inf there); done_out (nullable) [B, W]: 1 where the label is eos.
+ * A logit of -inf is a label that is not proposed.  A row that holds a NaN or +inf, or nothing but -inf, proposes nothing.
+ * Sums, scores and comparisons are carried out in double (exponentials in fp32), whatever dtype is; proposals whose score
+ * lies below the range of fp32 are none.  W <= 32, V < 2^31.  No output may be an input.
+ *   workspace: q4_workspace_bytes(Q4_WS_LM_SELECT, {B, W, V}) bytes, not cleared; calls that overlap need one each.
+ */
+int q4_lm_beam_select(const void* logits, int64_t logits_stride, int32_t dtype, const float* score, const uint8_t* done,
+                      int32_t B, int32_t W, int32_t V, int32_t eos, float rho, int32_t* parent, int32_t* token,
+                      float* score_out, uint8_t* done_out, void* workspace, size_t workspace_bytes, q4_stream stream);
+
+/*
+ * q4_beam_reorder — moves per-beam states to the beams that continue them: row (b, w) of dst becomes row (b, parent[b, w]) of
+ * src, for up to Q4_REORDER_MAX tensors in one launch; where parent is negative (or not below W) the row of dst is left as it was.
+ * A tensor is a set of rows of row_bytes contiguous bytes at
+ *   base + i0 step[0] + i1 step[1] + (b W + w) row_step,  i0 < n[0], i1 < n[1]   (bytes; steps of src and dst of their own):
+ * n[0] for what lies outside the beams (layers), n[1] for what lies inside (heads), so that the used part of a cache can be
+ * moved and the rest left alone.  Steps are not negative, those of dst no shorter than a row.  No dst may overlap a src of the
+ * call (Q4_ERR_UNSUPPORTED, judged by the range from a tensor's first to its last byte), and rows of dst lie apart;
+ * parent [B, W] (device).
+ */
+#define Q4_REORDER_MAX 16
+typedef struct {
+  const void* src;
+  void* dst;
+  int64_t row_bytes, src_row_step, dst_row_step;
+  int64_t n[2], src_step[2], dst_step[2];
+} q4_reorder;
+int q4_beam_reorder(const q4_reorder* items, int32_t n_items, const int32_t* parent, int32_t B, int32_t W, q4_stream stream);
+
 #define Q4_WS_LSTM_LAYER 1 /* dims = {T, B, dirs, H} or {T, B, dirs, H, kx_pad} */
 #define Q4_WS_JOINT 2      /* dims = {N, D} or {N, D, Hp_pad} (tensor-core path) */
 #define Q4_WS_BEAM 3       /* dims = {B, W, V, D}, {B, W, V, D, E_pad, Hp, Hs, Ht} or the latter and the state rows per utterance */
 #define Q4_WS_LSTM_STEP 4  /* dims = {N, kx_pad, H} (tensor-core path of qlstm_step) */
 #define Q4_WS_LINEAR 5     /* dims = {M, k_pad} (tensor-core path of q4_linear_forward) */
+#define Q4_WS_LM_SELECT 6  /* dims = {B, W, V} */
 size_t q4_workspace_bytes(int32_t call_id, const int32_t* dims, int32_t ndims);
 
 /* Synchronise `stream`, read the device status word and return 0 or the error it holds. */
@@ -483,7 +564,8 @@ int q4_test_wait_expiry_set(int32_t skip_producer, uint32_t wait_limit);
  * encoder input GEMM, 3 encoder recurrent step, 4 linear, 5 prediction LSTM, 6 prediction
  * projection, 7 source-LM LSTM, 8 source-LM head, 9 target-LM layer 1, 10 target-LM layer 2,
  * 11 target-LM head, 12 joint, 13 beam selection, 14 other, 15 first layers of a search that looks
- * labels up, 16 its recurrent sums. */
+ * labels up, 16 its recurrent sums, 17 norm, 18 linear with token scales, 19 beam selection over a vocabulary,
+ * 20 reordering of states. */
 int q4_timing_set(uint32_t tag_mask, void** start_events, void** stop_events, int32_t* tags_out,
                   int32_t capacity);
 int q4_timing_count(void);

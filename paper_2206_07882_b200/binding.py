@@ -20,7 +20,9 @@ LIB_PATH = os.path.join(_HERE, "libq4rnnt.so")
 
 ERRORS = {-1: "Q4_ERR_NULL", -2: "Q4_ERR_DIM", -3: "Q4_ERR_ALIGN", -4: "Q4_ERR_BITS",
           -5: "Q4_ERR_WORKSPACE", -6: "Q4_ERR_UNSUPPORTED", -7: "Q4_ERR_CUDA", -8: "Q4_ERR_TIMEOUT"}
-WS_LSTM_LAYER, WS_JOINT, WS_BEAM, WS_LSTM_STEP, WS_LINEAR = 1, 2, 3, 4, 5
+WS_LSTM_LAYER, WS_JOINT, WS_BEAM, WS_LSTM_STEP, WS_LINEAR, WS_LM_SELECT = 1, 2, 3, 4, 5, 6
+DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}      # Q4_F32, Q4_F16, Q4_BF16
+REORDER_MAX = 16
 
 
 class Q4Error(RuntimeError):
@@ -78,11 +80,18 @@ class BeamStateS(C.Structure):
                 ("nb_prev_hash", C.c_void_p), ("nb_n", C.c_void_p)]
 
 
+class ReorderS(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("row_bytes", C.c_int64), ("src_row_step", C.c_int64),
+                ("dst_row_step", C.c_int64), ("n", C.c_int64 * 2), ("src_step", C.c_int64 * 2),
+                ("dst_step", C.c_int64 * 2)]
+
+
 EXPORTS = ["q4_act_symmetric", "q4_act_asymmetric", "quantize_pack_int4", "qlstm_layer_forward",
            "qlstm_step", "q4_linear_forward", "qjoint_logprobs", "q4_beam_init",
            "dr_fusion_beam_step", "q4_beam_search", "q4_search_plan_create", "q4_search_plan_destroy", "q4_search_plan_info", "q4_search_steps_taken", "q4_traceback", "q4_feature_prologue", "q4_workspace_bytes",
            "q4_poll_status", "q4_version", "q4_launch_count", "q4_dependent_launch_set", "q4_beam_select_exact_set", "q4_timing_set", "q4_timing_count", "q4_prepared_bytes", "q4_prepare_model", "q4_table_bytes", "q4_prepare_tables", "qjoint_logprobs_static", "q4_quantizer_calls", "q4_prepared_lstm_bytes", "q4_prepare_lstm",
-           "q4_prepared_linear_bytes", "q4_prepare_linear", "q4_test_wait_expiry_set", "q4_test_search_loop_failure_set", "q4_encoder_time_slicing_set", "q4_encoder_recurrence_plan"]
+           "q4_prepared_linear_bytes", "q4_prepare_linear", "q4_test_wait_expiry_set", "q4_test_search_loop_failure_set", "q4_encoder_time_slicing_set", "q4_encoder_recurrence_plan",
+           "q4_rmsnorm_quantize", "q4_linear_token_scales", "q4_lm_beam_select", "q4_beam_reorder"]
 
 _lib = None
 
@@ -155,6 +164,18 @@ def _scratch(owner, rows: int, stream: int, call_id: int, dims: tuple, device) -
 def _chk(code: int, where: str):
     if code != 0:
         raise Q4Error(code, where)
+
+
+def _require(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _on_device(*tensors: Optional[torch.Tensor]):
+    """The library launches on the current device and stream: all tensors of a call have to be there."""
+    for t in tensors:
+        _require(t is None or (t.is_cuda and t.device.index == torch.cuda.current_device()),
+                 "tensors must be on the current CUDA device")
 
 
 def pad32(k: int) -> int:
@@ -324,11 +345,22 @@ class DeviceLstm:
 
 class DeviceLinear:
     def __init__(self, lw, device="cuda"):
-        self.w = DeviceMat.from_codes(lw.w.codes, lw.w.scale, lw.w.bits, device)
-        self.bias = _dev_f32(lw.bias, device)
+        self._hold(DeviceMat.from_codes(lw.w.codes, lw.w.scale, lw.w.bits, device), _dev_f32(lw.bias, device))
+
+    def _hold(self, w: DeviceMat, bias: Optional[torch.Tensor]):
+        self.w, self.bias = w, bias
         self.prepared = None
         self.ws = None            # the workspace of the last call (its first word is the call's status)
         self.stream_ws = {}
+
+    @staticmethod
+    def from_mat(w: DeviceMat, bias: Optional[torch.Tensor] = None) -> "DeviceLinear":
+        """A layer over weights that are on the device already (DeviceMat.from_float_max, for instance)."""
+        lin = DeviceLinear.__new__(DeviceLinear)
+        _require(bias is None or (bias.dtype == torch.float32 and bias.shape == (w.rows,) and bias.is_contiguous()
+                                  and bias.device == w.q.device), "bias: one contiguous fp32 value per weight row, beside the weights")
+        lin._hold(w, bias)
+        return lin
 
     def prepare(self):
         """One-time int8 operand for the tensor-core paths (q4_prepare_linear)."""
@@ -491,6 +523,138 @@ def q4_feature_prologue(mel: torch.Tensor) -> torch.Tensor:
     _chk(lib().q4_feature_prologue(_p(mel), C.c_int32(B), C.c_int32(T100), C.c_int32(M), _p(out),
                                    _stream()), "q4_feature_prologue")
     return out
+
+
+# ------------------------------------------------------------------ around the output of a language model
+def _rows(t: torch.Tensor, k: int, what: str) -> int:
+    """Distance of the rows of a [rows, k] tensor in elements; a single row has any."""
+    _require(t.dim() == 2 and t.shape[1] == k and (k == 1 or t.stride(1) == 1), f"{what}: [rows, {k}] with contiguous rows")
+    return max(t.stride(0), k) if t.shape[0] > 1 else k
+
+
+def q4_rmsnorm_quantize(x: torch.Tensor, gain: torch.Tensor, eps: float, residual: Optional[torch.Tensor] = None,
+                        sum_out: Optional[torch.Tensor] = None, k_pad: Optional[int] = None):
+    """x [rows, k] -> (codes [rows, k_pad] uint8 holding int8, scale [rows]); with `residual` the norm is taken of x + residual,
+    which is written to `sum_out` (x or residual itself, or another tensor)."""
+    _need_cuda()
+    _require(x.dim() == 2 and x.dtype in DTYPES, "x: [rows, k] of fp32, fp16 or bf16")
+    rows, k = x.shape
+    _on_device(x, gain, residual, sum_out)
+    _require(gain.dtype == torch.float32 and gain.shape == (k,) and gain.is_contiguous(), "gain: k contiguous fp32 values")
+    _require((residual is None) == (sum_out is None), "sum_out goes with a residual")
+    for t, name in ((residual, "residual"), (sum_out, "sum_out")):
+        _require(t is None or (t.dtype == x.dtype and t.shape == x.shape), f"{name}: like x")
+    ld = [0 if t is None else _rows(t, k, "x, residual and sum_out") for t in (x, residual, sum_out)]
+    for t in (x, residual, sum_out):
+        _require(t is None or rows < 2 or t.stride(0) >= k, "rows must not overlap")
+    k_pad = pad32(k) if k_pad is None else k_pad
+    q = torch.empty((rows, k_pad), dtype=torch.uint8, device=x.device)
+    scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    _chk(lib().q4_rmsnorm_quantize(_p(x), C.c_int64(ld[0]), _p(residual), C.c_int64(ld[1]), C.c_int32(DTYPES[x.dtype]),
+                                   C.c_int64(rows), C.c_int32(k), C.c_int32(k_pad), _p(gain), C.c_float(eps), _p(sum_out),
+                                   C.c_int64(ld[2]), _p(q), _p(scale), _stream()), "q4_rmsnorm_quantize")
+    return q, scale
+
+
+def q4_linear_token_scales(xq: torch.Tensor, x_scale: torch.Tensor, lin: DeviceLinear,
+                           out_dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None,
+                           status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Codes [M, k_pad] with one scale per row times 8-bit weights -> [M, rows of the weights] of out_dtype (or `out`, whose
+    rows may lie further apart).  `status`: one int32, zero before the first call (q4_poll_status)."""
+    _need_cuda()
+    M = xq.shape[0]
+    w = lin.w
+    _on_device(xq, x_scale, w.q, out, status)
+    _require(xq.dim() == 2 and xq.element_size() == 1 and xq.is_contiguous() and xq.shape[1] == w.k_pad,
+             "xq: contiguous 8-bit codes in rows as long as the weights'")
+    _require(x_scale.dtype == torch.float32 and x_scale.shape == (M,) and x_scale.is_contiguous(), "x_scale: one fp32 per row")
+    if out is None:
+        _require(out_dtype in DTYPES, "out_dtype: fp32, fp16 or bf16")
+        out = torch.empty((M, w.rows), dtype=out_dtype, device=xq.device)
+    _require(out.dtype in DTYPES and out.shape[:1] == (M,), "out: [M, rows of the weights] of fp32, fp16 or bf16")
+    ld = _rows(out, w.rows, "out")
+    _require(M < 2 or out.stride(0) >= w.rows, "rows of out must not overlap")
+    m = w.c()
+    _chk(lib().q4_linear_token_scales(_p(xq), _p(x_scale), C.c_int32(M), C.byref(m), _p(lin.bias), _p(out),
+                                      C.c_int32(DTYPES[out.dtype]), C.c_int64(ld), _p(status), _stream()),
+         "q4_linear_token_scales")
+    return out
+
+
+def q4_lm_beam_select(logits: torch.Tensor, score: torch.Tensor, done: Optional[torch.Tensor] = None, eos: int = -1,
+                      rho: float = 0.0, workspace: Optional[torch.Tensor] = None) -> dict:
+    """One step of a label-synchronous beam search: logits [B, W, V], score [B, W] fp32, done [B, W] uint8 or bool (beams
+    that have ended) -> dict(parent, token [B, W] int32, score [B, W], done [B, W] uint8).  `workspace`: bytes of
+    workspace_bytes(WS_LM_SELECT, (B, W, V)) of the caller's own; without one the call allocates it."""
+    _need_cuda()
+    _require(logits.dim() == 3 and logits.dtype in DTYPES, "logits: [B, W, V] of fp32, fp16 or bf16")
+    B, W, V = logits.shape
+    _on_device(logits, score, done, workspace)
+    _require(score.dtype == torch.float32 and score.shape == (B, W) and score.is_contiguous(), "score: contiguous fp32 [B, W]")
+    _require(done is None or (done.element_size() == 1 and done.shape == (B, W) and done.is_contiguous()),
+             "done: contiguous bytes [B, W]")
+    _require(V == 1 or logits.stride(2) == 1, "logits: contiguous rows")
+    ld = logits.stride(1) if W > 1 else logits.stride(0) if B > 1 else V
+    _require(B * W < 2 or (ld >= V and (B < 2 or logits.stride(0) == W * ld)), "logits: rows at one distance, beams within utterances")
+    dev = logits.device
+    r = {"parent": torch.empty((B, W), dtype=torch.int32, device=dev), "token": torch.empty((B, W), dtype=torch.int32, device=dev),
+         "score": torch.empty((B, W), dtype=torch.float32, device=dev), "done": torch.empty((B, W), dtype=torch.uint8, device=dev)}
+    need = workspace_bytes(WS_LM_SELECT, (B, W, V))
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    _chk(lib().q4_lm_beam_select(_p(logits), C.c_int64(max(ld, V)), C.c_int32(DTYPES[logits.dtype]), _p(score), _p(done), C.c_int32(B),
+                                 C.c_int32(W), C.c_int32(V), C.c_int32(eos), C.c_float(rho), _p(r["parent"]), _p(r["token"]),
+                                 _p(r["score"]), _p(r["done"]), _p(workspace), C.c_size_t(workspace.numel()), _stream()),
+         "q4_lm_beam_select")
+    return r
+
+
+def _reorder_item(t: ReorderS, src: torch.Tensor, dst: torch.Tensor, dim: int, B: int, W: int):
+    """Rows, steps and counts of a pair of tensors whose dimensions `dim` and `dim + 1` are utterance and beam."""
+    _require(src.dtype == dst.dtype and src.shape == dst.shape and src.dim() >= dim + 2 and tuple(src.shape[dim:dim + 2]) == (B, W),
+             "src and dst: alike, with utterances and beams as dimensions dim and dim + 1")
+    es, shape = src.element_size(), src.shape
+    strides = [[s * es for s in x.stride()] for x in (src, dst)]
+    for s in strides:
+        _require(B < 2 or W < 2 or s[dim] == W * s[dim + 1], "rows of one utterance must follow those of the one before")
+    row = [s[dim + 1] if W > 1 else s[dim] for s in strides]
+    inner = list(range(dim + 2, src.dim()))
+    row_bytes = es
+    while inner and all(s[inner[-1]] == row_bytes or shape[inner[-1]] == 1 for s in strides):   # contiguous in both
+        row_bytes *= shape[inner.pop()]
+
+    def one(dims):           # several dimensions that are one in both tensors, as (count, steps)
+        n, step = 1, [0, 0]
+        for d in reversed(dims):
+            if shape[d] != 1:
+                _require(n == 1 or all(s[d] == n * p for s, p in zip(strides, step)), "too many dimensions that are not contiguous")
+                if n == 1:
+                    step = [s[d] for s in strides]
+                n *= shape[d]
+        return n, step
+
+    (n0, s0), (n1, s1) = one(range(dim)), one(inner)
+    t.src, t.dst, t.row_bytes = src.data_ptr(), dst.data_ptr(), row_bytes if src.numel() else 0
+    t.src_row_step, t.dst_row_step = row
+    t.n[0], t.n[1] = n0, n1
+    t.src_step[0], t.src_step[1], t.dst_step[0], t.dst_step[1] = s0[0], s1[0], s0[1], s1[1]
+
+
+def q4_beam_reorder(pairs: Sequence, parent: torch.Tensor, dim: int = 0):
+    """dst[..., b, w, ...] = src[..., b, parent[b, w], ...] for pairs (src, dst) of tensors whose dimensions `dim` and `dim` + 1
+    are utterance and beam; where parent is negative dst is left as it was.  Views are fine (the used part of a cache)."""
+    _need_cuda()
+    _require(parent.dim() == 2 and parent.dtype == torch.int32 and parent.is_contiguous(), "parent: contiguous int32 [B, W]")
+    B, W = parent.shape
+    _require(W > 0 or not pairs, "parent: at least one beam")
+    for first in range(0, len(pairs), REORDER_MAX):
+        group = pairs[first:first + REORDER_MAX]
+        items = (ReorderS * len(group))()
+        for item, (src, dst) in zip(items, group):
+            _on_device(parent, src, dst)
+            _reorder_item(item, src, dst, dim, B, W)
+        _chk(lib().q4_beam_reorder(items, C.c_int32(len(group)), _p(parent), C.c_int32(B), C.c_int32(W), _stream()),
+             "q4_beam_reorder")
 
 
 # ------------------------------------------------------------------ whole networks

@@ -231,6 +231,8 @@ size_t q4_workspace_bytes(int32_t call_id, const int32_t* dims, int32_t ndims) {
     }
     return n;
   }
+  if (call_id == Q4_WS_LM_SELECT && ndims >= 3 && dims[0] >= 0 && dims[1] > 0 && dims[2] > 0)
+    return lm_select_workspace(dims[0], dims[1], dims[2]);
   return 0;
 }
 
@@ -1872,6 +1874,153 @@ int q4_traceback(const q4_beam_state* state, int32_t B, int32_t W, int32_t n_ite
   if (!tokens || !lens || !scores) return Q4_ERR_NULL;
   if (B <= 0 || W <= 0 || W > 16 || n_iters < 0 || u_max <= 0) return Q4_ERR_DIM;
   Q4_TRY(launch_traceback(*state, B, W, n_iters, u_max, tokens, lens, scores, S(stream)));
+  return Q4_OK;
+}
+
+
+// ---- around the output of a language model
+static int element_bytes(int32_t dtype) { return dtype == Q4_F32 ? 4 : dtype == Q4_F16 || dtype == Q4_BF16 ? 2 : 0; }
+static bool aligned_to(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % (unsigned)bytes == 0; }
+
+int q4_rmsnorm_quantize(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, int32_t dtype,
+                        int64_t rows, int32_t k, int32_t k_pad, const float* gain, float eps, void* sum_out,
+                        int64_t sum_stride, void* q_out, float* scale_out, q4_stream stream) {
+  const int es = element_bytes(dtype);
+  if (!es) return Q4_ERR_UNSUPPORTED;
+  if (rows < 0 || k <= 0 || k_pad < k || x_stride < k) return Q4_ERR_DIM;
+  if (!(eps >= 0.0f) || isinf(eps)) return Q4_ERR_DIM;
+  if (rows > 0 && (!x || !gain || !q_out || !scale_out)) return Q4_ERR_NULL;
+  if (!residual != !sum_out) return rows > 0 ? Q4_ERR_NULL : Q4_OK;
+  if (residual && (residual_stride < k || sum_stride < k)) return Q4_ERR_DIM;
+  if (residual && ((sum_out == x && sum_stride != x_stride) || (sum_out == residual && sum_stride != residual_stride)))
+    return Q4_ERR_UNSUPPORTED;
+  if (k_pad % 32 != 0 || !aligned16(q_out) || !aligned_to(x, es) || !aligned_to(residual, es) || !aligned_to(sum_out, es) ||
+      !aligned_to(gain, 4) || !aligned_to(scale_out, 4))
+    return Q4_ERR_ALIGN;
+  if (rows == 0) return Q4_OK;
+  NormArgs a;
+  memset(&a, 0, sizeof(a));
+  a.x = x;
+  a.residual = residual;
+  a.sum = sum_out;
+  a.x_ld = x_stride;
+  a.r_ld = residual_stride;
+  a.s_ld = sum_stride;
+  a.rows = rows;
+  a.k = k;
+  a.k_pad = k_pad;
+  a.gain = gain;
+  a.eps = eps;
+  a.q = static_cast<int8_t*>(q_out);
+  a.scale = scale_out;
+  TagScope tag(TAG_NORM);
+  Q4_TRY(launch_rmsnorm_quantize(a, dtype, S(stream)));
+  ++g_quant_calls;
+  return Q4_OK;
+}
+
+int q4_linear_token_scales(const void* xq, const float* x_scale, int32_t M, const q4_mat* w, const float* bias, void* out,
+                           int32_t out_dtype, int64_t out_stride, int32_t* status, q4_stream stream) {
+  const int es = element_bytes(out_dtype);
+  if (!es) return Q4_ERR_UNSUPPORTED;
+  Q4_CHECK(check_mat(w, 0, 0));
+  if (w->bits != 8) return Q4_ERR_BITS;
+  if (M < 0 || w->k_pad > 131040 || out_stride < w->rows) return Q4_ERR_DIM;
+  if (M > 0 && (!xq || !x_scale || !out)) return Q4_ERR_NULL;
+  if (!aligned16(xq) || !aligned_to(x_scale, 4) || !aligned_to(bias, 4) || !aligned_to(out, es) || !aligned_to(status, 4))
+    return Q4_ERR_ALIGN;
+  if (M == 0) return Q4_OK;
+  TokenLinearArgs a;
+  memset(&a, 0, sizeof(a));
+  a.xq = static_cast<const int8_t*>(xq);
+  a.x_scale = x_scale;
+  a.wq = static_cast<const int8_t*>(w->q);
+  a.w_scale = w->scale;
+  a.bias = bias;
+  a.out = out;
+  a.ldo = out_stride;
+  a.M = M;
+  a.N = w->rows;
+  a.K = w->k_pad;
+  a.status = status;
+  TagScope tag(TAG_TOKEN_LINEAR);
+  Q4_TRY(launch_token_linear(a, out_dtype, S(stream)));
+  return Q4_OK;
+}
+
+int q4_lm_beam_select(const void* logits, int64_t logits_stride, int32_t dtype, const float* score, const uint8_t* done,
+                      int32_t B, int32_t W, int32_t V, int32_t eos, float rho, int32_t* parent, int32_t* token,
+                      float* score_out, uint8_t* done_out, void* workspace, size_t workspace_bytes, q4_stream stream) {
+  const int es = element_bytes(dtype);
+  if (!es) return Q4_ERR_UNSUPPORTED;
+  if (B < 0 || W <= 0 || W > 32 || V <= 0 || logits_stride < V || (int64_t)B * W > INT32_MAX) return Q4_ERR_DIM;
+  if (eos < -1 || eos >= V || (done && eos < 0) || !isfinite(rho)) return Q4_ERR_DIM;
+  if (B == 0) return Q4_OK;
+  if (!logits || !score || !parent || !token || !score_out || !workspace) return Q4_ERR_NULL;
+  if (score_out == score || (done && done_out == done)) return Q4_ERR_UNSUPPORTED;
+  if (!aligned_to(logits, es) || !aligned_to(score, 4) || !aligned_to(parent, 4) || !aligned_to(token, 4) ||
+      !aligned_to(score_out, 4) || !aligned16(workspace))
+    return Q4_ERR_ALIGN;
+  const int32_t wd[3] = {B, W, V};
+  if (workspace_bytes < q4_workspace_bytes(Q4_WS_LM_SELECT, wd, 3)) return Q4_ERR_WORKSPACE;
+  LmSelectArgs a;
+  memset(&a, 0, sizeof(a));
+  a.logits = logits;
+  a.ld = logits_stride;
+  a.score = score;
+  a.done = done;
+  a.B = B;
+  a.W = W;
+  a.V = V;
+  a.eos = eos;
+  a.rho = rho;
+  a.parent = parent;
+  a.token = token;
+  a.score_out = score_out;
+  a.done_out = done_out;
+  a.workspace = static_cast<uint8_t*>(workspace);
+  TagScope tag(TAG_LM_SELECT);
+  Q4_TRY(launch_lm_select(a, dtype, S(stream)));
+  return Q4_OK;
+}
+
+// First and one past the last byte of an item's rows in memory; false: the sizes overflow.
+static bool reorder_extent(const void* base, const q4_reorder& t, int64_t row_step, const int64_t* step, int64_t rows, uint64_t* lo,
+                           uint64_t* hi) {
+  const int64_t most = (int64_t)1 << 47;   // of an address
+  __int128 n = (__int128)(rows - 1) * row_step + t.row_bytes;
+  for (int d = 0; d < 2; ++d) n += (__int128)(t.n[d] - 1) * step[d];
+  if (n > most) return false;
+  *lo = reinterpret_cast<uintptr_t>(base);
+  *hi = *lo + (uint64_t)n;
+  return true;
+}
+
+int q4_beam_reorder(const q4_reorder* items, int32_t n_items, const int32_t* parent, int32_t B, int32_t W, q4_stream stream) {
+  if (n_items < 0 || n_items > Q4_REORDER_MAX || B < 0 || W <= 0 || (int64_t)B * W > INT32_MAX) return Q4_ERR_DIM;
+  if (n_items == 0 || B == 0) return Q4_OK;
+  if (!items || !parent) return Q4_ERR_NULL;
+  if (!aligned_to(parent, 4)) return Q4_ERR_ALIGN;
+  const int64_t rows = (int64_t)B * W;
+  uint64_t lo[2][Q4_REORDER_MAX], hi[2][Q4_REORDER_MAX];   // src, dst
+  for (int i = 0; i < n_items; ++i) {
+    const q4_reorder& t = items[i];
+    if (t.row_bytes < 0 || t.n[0] < 0 || t.n[1] < 0 || t.src_row_step < 0 || t.dst_row_step < 0) return Q4_ERR_DIM;
+    lo[0][i] = hi[0][i] = lo[1][i] = hi[1][i] = 0;
+    if (t.row_bytes == 0 || t.n[0] == 0 || t.n[1] == 0) continue;
+    if (!t.src || !t.dst) return Q4_ERR_NULL;
+    if (rows > 1 && t.dst_row_step < t.row_bytes) return Q4_ERR_DIM;
+    for (int d = 0; d < 2; ++d)
+      if (t.src_step[d] < 0 || t.dst_step[d] < 0 || (t.n[d] > 1 && t.dst_step[d] < t.row_bytes)) return Q4_ERR_DIM;
+    if (!reorder_extent(t.src, t, t.src_row_step, t.src_step, rows, &lo[0][i], &hi[0][i]) ||
+        !reorder_extent(t.dst, t, t.dst_row_step, t.dst_step, rows, &lo[1][i], &hi[1][i]))
+      return Q4_ERR_DIM;
+  }
+  for (int i = 0; i < n_items; ++i)
+    for (int j = 0; j < n_items; ++j)
+      if (lo[1][i] < hi[0][j] && lo[0][j] < hi[1][i]) return Q4_ERR_UNSUPPORTED;
+  TagScope tag(TAG_REORDER);
+  Q4_TRY(launch_beam_reorder(items, n_items, parent, B, W, S(stream)));
   return Q4_OK;
 }
 

@@ -70,7 +70,8 @@ cudaError_t launch_traceback(const q4_beam_state& st, int B, int W, int n_iters,
 enum { TAG_NONE = 0, TAG_QUANT = 1, TAG_ENC_GEMM = 2, TAG_ENC_STEP = 3, TAG_LINEAR = 4,
        TAG_PRED_LSTM = 5, TAG_PRED_PROJ = 6, TAG_SRC_LSTM = 7, TAG_SRC_HEAD = 8, TAG_TGT_L1 = 9,
        TAG_TGT_L2 = 10, TAG_TGT_HEAD = 11, TAG_JOINT = 12, TAG_SELECT = 13, TAG_MISC = 14,
-       TAG_CELLS = 15, TAG_STATE = 16, TAG_COUNT = 17 };
+       TAG_CELLS = 15, TAG_STATE = 16, TAG_NORM = 17, TAG_TOKEN_LINEAR = 18, TAG_LM_SELECT = 19, TAG_REORDER = 20,
+       TAG_COUNT = 21 };
 extern int g_tag;   // tag of the launches being issued
 struct TagScope {
   int prev;
@@ -310,6 +311,49 @@ struct EncRecPlan {
 EncRecPlan enc_recurrent_plan(int T, int B, int dirs, int H, int w_bits, int hid_bits, bool hid_signed,
                               bool per_sequence_scale, bool dump, bool scratch);
 cudaError_t launch_enc_recurrent(EncRecArgs a, cudaStream_t s);
+
+// ---- around the output of a language model (q4_norm.cu, q4_token_linear.cu, q4_lm_search.cu)
+struct NormArgs {
+  const void* x;
+  const void* residual;     // nullable
+  void* sum;                // with residual
+  long long x_ld, r_ld, s_ld;   // elements between rows
+  long long rows;
+  int32_t k, k_pad;
+  const float* gain;
+  float eps;
+  int8_t* q;                // [rows, k_pad]
+  float* scale;
+};
+cudaError_t launch_rmsnorm_quantize(const NormArgs& a, int dtype, cudaStream_t s);
+struct TokenLinearArgs {
+  const int8_t* xq;         // [M, K] codes
+  const float* x_scale;     // [M]
+  const int8_t* wq;         // [N, K]
+  const float* w_scale;     // [N]
+  const float* bias;        // nullable
+  void* out;
+  long long ldo;
+  int32_t M, N, K;          // K: padded row length
+  int32_t* status;          // nullable
+};
+cudaError_t launch_token_linear(const TokenLinearArgs& a, int dtype, cudaStream_t s);
+struct LmSelectArgs {
+  const void* logits;
+  long long ld;             // elements between rows
+  const float* score;
+  const uint8_t* done;      // nullable
+  int32_t B, W, V, eos;
+  float rho;
+  int32_t* parent;
+  int32_t* token;
+  float* score_out;
+  uint8_t* done_out;        // nullable
+  uint8_t* workspace;
+};
+size_t lm_select_workspace(int B, int W, int V);
+cudaError_t launch_lm_select(const LmSelectArgs& a, int dtype, cudaStream_t s);
+cudaError_t launch_beam_reorder(const q4_reorder* items, int n_items, const int32_t* parent, int B, int W, cudaStream_t s);
 
 inline size_t align_up(size_t v, size_t a = 256) { return (v + a - 1) / a * a; }
 
