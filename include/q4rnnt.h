@@ -464,11 +464,13 @@ int q4_linear_token_scales(const void* xq, const float* x_scale, int32_t M, cons
  * A logit of -inf is a label that is not proposed.  A row that holds a NaN or +inf, or nothing but -inf, proposes nothing.
  * Sums, scores and comparisons are carried out in double (exponentials in fp32), whatever dtype is; proposals whose score
  * lies below the range of fp32 are none.  W <= 32, V < 2^31.  No output may be an input.
- *   workspace: q4_workspace_bytes(Q4_WS_LM_SELECT, {B, W, V}) bytes, not cleared; calls that overlap need one each.
+ *   arrived [B]: counters, zero before the first call; every call leaves them zero.  workspace: q4_workspace_bytes(
+ *   Q4_WS_LM_SELECT, {B, W, V}) bytes, any contents.  Calls that may overlap need counters and a workspace each.
  */
 int q4_lm_beam_select(const void* logits, int64_t logits_stride, int32_t dtype, const float* score, const uint8_t* done,
                       int32_t B, int32_t W, int32_t V, int32_t eos, float rho, int32_t* parent, int32_t* token,
-                      float* score_out, uint8_t* done_out, void* workspace, size_t workspace_bytes, q4_stream stream);
+                      float* score_out, uint8_t* done_out, uint32_t* arrived, void* workspace, size_t workspace_bytes,
+                      q4_stream stream);
 
 /*
  * q4_beam_reorder — moves per-beam states to the beams that continue them: row (b, w) of dst becomes row (b, parent[b, w]) of

@@ -111,6 +111,12 @@ def lib() -> C.CDLL:
         _lib.q4_quantizer_calls.restype = C.c_int64
         _lib.q4_prepared_lstm_bytes.restype = C.c_size_t
         _lib.q4_prepared_linear_bytes.restype = C.c_size_t
+        # calls of a few microseconds: their arguments are converted without an object for each
+        v, i, j, f, z = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_size_t
+        _lib.q4_rmsnorm_quantize.argtypes = [v, j, v, j, i, j, i, i, v, f, v, j, v, v, v]
+        _lib.q4_linear_token_scales.argtypes = [v, v, i, C.POINTER(Mat), v, v, i, j, v, v]
+        _lib.q4_lm_beam_select.argtypes = [v, j, i, v, v, i, i, i, i, f, v, v, v, v, v, v, z, v]
+        _lib.q4_beam_reorder.argtypes = [C.POINTER(ReorderS), i, v, i, i, v]
     return _lib
 
 
@@ -171,11 +177,18 @@ def _require(ok: bool, what: str):
         raise ValueError(what)
 
 
-def _on_device(*tensors: Optional[torch.Tensor]):
-    """The library launches on the current device and stream: all tensors of a call have to be there."""
-    for t in tensors:
-        _require(t is None or (t.is_cuda and t.device.index == torch.cuda.current_device()),
-                 "tensors must be on the current CUDA device")
+def _on_device(first: Optional[torch.Tensor], *others: Optional[torch.Tensor]) -> int:
+    """The library launches on the current device and stream: all tensors of a call have to be there.  Returns its index."""
+    d = first.get_device() if first is not None else -1
+    ok = first is None or (d >= 0 and d == torch._C._cuda_getDevice())
+    for t in others:
+        ok = ok and (t is None or t.get_device() == d)
+    _require(ok, "tensors must be on the current CUDA device")
+    return d
+
+
+def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
 
 
 def pad32(k: int) -> int:
@@ -526,10 +539,13 @@ def q4_feature_prologue(mel: torch.Tensor) -> torch.Tensor:
 
 
 # ------------------------------------------------------------------ around the output of a language model
-def _rows(t: torch.Tensor, k: int, what: str) -> int:
+# (calls of a few microseconds: plain checks, no objects that are not needed)
+def _rows(t: torch.Tensor, rows: int, k: int, what: str) -> int:
     """Distance of the rows of a [rows, k] tensor in elements; a single row has any."""
-    _require(t.dim() == 2 and t.shape[1] == k and (k == 1 or t.stride(1) == 1), f"{what}: [rows, {k}] with contiguous rows")
-    return max(t.stride(0), k) if t.shape[0] > 1 else k
+    s = t.stride()
+    if t.shape != (rows, k) or (s[1] != 1 and k > 1) or (s[0] < k and rows > 1):
+        raise ValueError(f"{what}: [{rows}, {k}], rows contiguous and apart")
+    return s[0] if rows > 1 else k
 
 
 def q4_rmsnorm_quantize(x: torch.Tensor, gain: torch.Tensor, eps: float, residual: Optional[torch.Tensor] = None,
@@ -537,22 +553,27 @@ def q4_rmsnorm_quantize(x: torch.Tensor, gain: torch.Tensor, eps: float, residua
     """x [rows, k] -> (codes [rows, k_pad] uint8 holding int8, scale [rows]); with `residual` the norm is taken of x + residual,
     which is written to `sum_out` (x or residual itself, or another tensor)."""
     _need_cuda()
-    _require(x.dim() == 2 and x.dtype in DTYPES, "x: [rows, k] of fp32, fp16 or bf16")
+    dtype = x.dtype
+    if x.dim() != 2 or dtype not in DTYPES:
+        raise ValueError("x: [rows, k] of fp32, fp16 or bf16")
     rows, k = x.shape
-    _on_device(x, gain, residual, sum_out)
-    _require(gain.dtype == torch.float32 and gain.shape == (k,) and gain.is_contiguous(), "gain: k contiguous fp32 values")
-    _require((residual is None) == (sum_out is None), "sum_out goes with a residual")
-    for t, name in ((residual, "residual"), (sum_out, "sum_out")):
-        _require(t is None or (t.dtype == x.dtype and t.shape == x.shape), f"{name}: like x")
-    ld = [0 if t is None else _rows(t, k, "x, residual and sum_out") for t in (x, residual, sum_out)]
-    for t in (x, residual, sum_out):
-        _require(t is None or rows < 2 or t.stride(0) >= k, "rows must not overlap")
-    k_pad = pad32(k) if k_pad is None else k_pad
-    q = torch.empty((rows, k_pad), dtype=torch.uint8, device=x.device)
-    scale = torch.empty(rows, dtype=torch.float32, device=x.device)
-    _chk(lib().q4_rmsnorm_quantize(_p(x), C.c_int64(ld[0]), _p(residual), C.c_int64(ld[1]), C.c_int32(DTYPES[x.dtype]),
-                                   C.c_int64(rows), C.c_int32(k), C.c_int32(k_pad), _p(gain), C.c_float(eps), _p(sum_out),
-                                   C.c_int64(ld[2]), _p(q), _p(scale), _stream()), "q4_rmsnorm_quantize")
+    dev = _on_device(x, gain, residual, sum_out)
+    if gain.dtype != torch.float32 or gain.shape != (k,) or not gain.is_contiguous():
+        raise ValueError("gain: k contiguous fp32 values")
+    if (residual is None) != (sum_out is None):
+        raise ValueError("sum_out goes with a residual")
+    ld_x, ld_r, ld_s = _rows(x, rows, k, "x"), 0, 0
+    if residual is not None:
+        if residual.dtype != dtype or sum_out.dtype != dtype:
+            raise ValueError("residual and sum_out: of x's type")
+        ld_r, ld_s = _rows(residual, rows, k, "residual"), _rows(sum_out, rows, k, "sum_out")
+    if k_pad is None:
+        k_pad = (k + 31) // 32 * 32
+    q = gain.new_empty((rows, k_pad), dtype=torch.uint8)
+    scale = gain.new_empty((rows,))
+    _chk(lib().q4_rmsnorm_quantize(x.data_ptr(), ld_x, _ptr(residual), ld_r, DTYPES[dtype], rows, k, k_pad, gain.data_ptr(), eps,
+                                   _ptr(sum_out), ld_s, q.data_ptr(), scale.data_ptr(), torch._C._cuda_getCurrentRawStream(dev)),
+         "q4_rmsnorm_quantize")
     return q, scale
 
 
@@ -562,65 +583,90 @@ def q4_linear_token_scales(xq: torch.Tensor, x_scale: torch.Tensor, lin: DeviceL
     """Codes [M, k_pad] with one scale per row times 8-bit weights -> [M, rows of the weights] of out_dtype (or `out`, whose
     rows may lie further apart).  `status`: one int32, zero before the first call (q4_poll_status)."""
     _need_cuda()
-    M = xq.shape[0]
     w = lin.w
-    _on_device(xq, x_scale, w.q, out, status)
-    _require(xq.dim() == 2 and xq.element_size() == 1 and xq.is_contiguous() and xq.shape[1] == w.k_pad,
-             "xq: contiguous 8-bit codes in rows as long as the weights'")
-    _require(x_scale.dtype == torch.float32 and x_scale.shape == (M,) and x_scale.is_contiguous(), "x_scale: one fp32 per row")
+    dev = _on_device(xq, x_scale, w.q, out, status)
+    if xq.dim() != 2 or xq.element_size() != 1 or not xq.is_contiguous() or xq.shape[1] != w.k_pad:
+        raise ValueError("xq: contiguous 8-bit codes in rows as long as the weights'")
+    M = xq.shape[0]
+    if x_scale.dtype != torch.float32 or x_scale.shape != (M,) or not x_scale.is_contiguous():
+        raise ValueError("x_scale: one fp32 per row")
     if out is None:
-        _require(out_dtype in DTYPES, "out_dtype: fp32, fp16 or bf16")
-        out = torch.empty((M, w.rows), dtype=out_dtype, device=xq.device)
-    _require(out.dtype in DTYPES and out.shape[:1] == (M,), "out: [M, rows of the weights] of fp32, fp16 or bf16")
-    ld = _rows(out, w.rows, "out")
-    _require(M < 2 or out.stride(0) >= w.rows, "rows of out must not overlap")
-    m = w.c()
-    _chk(lib().q4_linear_token_scales(_p(xq), _p(x_scale), C.c_int32(M), C.byref(m), _p(lin.bias), _p(out),
-                                      C.c_int32(DTYPES[out.dtype]), C.c_int64(ld), _p(status), _stream()),
+        if out_dtype not in DTYPES:
+            raise ValueError("out_dtype: fp32, fp16 or bf16")
+        out, ld = x_scale.new_empty((M, w.rows), dtype=out_dtype), w.rows
+    else:
+        out_dtype = out.dtype
+        if out_dtype not in DTYPES or out.dim() != 2:
+            raise ValueError("out: [M, rows of the weights] of fp32, fp16 or bf16")
+        ld = _rows(out, M, w.rows, "out")
+    if status is not None and (status.dtype != torch.int32 or status.numel() < 1):
+        raise ValueError("status: one int32")
+    _chk(lib().q4_linear_token_scales(xq.data_ptr(), x_scale.data_ptr(), M, w.c(), _ptr(lin.bias), out.data_ptr(),
+                                      DTYPES[out_dtype], ld, _ptr(status), torch._C._cuda_getCurrentRawStream(dev)),
          "q4_linear_token_scales")
     return out
+
+
+# Counters and workspaces of beam selections, one pair per device and stream: calls on one stream are ordered.  A capture gets
+# its own from the graph's memory.
+_select_scratch: dict = {}
+
+
+def _scratch_of_select(like: torch.Tensor, dev: int, stream: int, B: int, need: int) -> tuple:
+    entry = _select_scratch.get((dev, stream))
+    capturing = _capturing()
+    if capturing or entry is None or entry[0].shape[0] < B or entry[1].shape[0] < need:
+        new = like.new_zeros((max(B, 64),), dtype=torch.int32), like.new_empty((need,), dtype=torch.uint8)
+        if capturing:
+            return new
+        if entry is None and len(_select_scratch) >= _SCRATCH_STREAMS:
+            del _select_scratch[next(iter(_select_scratch))]
+        entry = _select_scratch[dev, stream] = new
+    return entry
 
 
 def q4_lm_beam_select(logits: torch.Tensor, score: torch.Tensor, done: Optional[torch.Tensor] = None, eos: int = -1,
                       rho: float = 0.0, workspace: Optional[torch.Tensor] = None) -> dict:
     """One step of a label-synchronous beam search: logits [B, W, V], score [B, W] fp32, done [B, W] uint8 or bool (beams
     that have ended) -> dict(parent, token [B, W] int32, score [B, W], done [B, W] uint8).  `workspace`: bytes of
-    workspace_bytes(WS_LM_SELECT, (B, W, V)) of the caller's own; without one the call allocates it."""
+    workspace_bytes(WS_LM_SELECT, (B, W, V)) of the caller's own."""
     _need_cuda()
-    _require(logits.dim() == 3 and logits.dtype in DTYPES, "logits: [B, W, V] of fp32, fp16 or bf16")
+    dtype = logits.dtype
+    if logits.dim() != 3 or dtype not in DTYPES:
+        raise ValueError("logits: [B, W, V] of fp32, fp16 or bf16")
     B, W, V = logits.shape
-    _on_device(logits, score, done, workspace)
-    _require(score.dtype == torch.float32 and score.shape == (B, W) and score.is_contiguous(), "score: contiguous fp32 [B, W]")
-    _require(done is None or (done.element_size() == 1 and done.shape == (B, W) and done.is_contiguous()),
-             "done: contiguous bytes [B, W]")
-    _require(V == 1 or logits.stride(2) == 1, "logits: contiguous rows")
-    ld = logits.stride(1) if W > 1 else logits.stride(0) if B > 1 else V
-    _require(B * W < 2 or (ld >= V and (B < 2 or logits.stride(0) == W * ld)), "logits: rows at one distance, beams within utterances")
-    dev = logits.device
-    r = {"parent": torch.empty((B, W), dtype=torch.int32, device=dev), "token": torch.empty((B, W), dtype=torch.int32, device=dev),
-         "score": torch.empty((B, W), dtype=torch.float32, device=dev), "done": torch.empty((B, W), dtype=torch.uint8, device=dev)}
-    need = workspace_bytes(WS_LM_SELECT, (B, W, V))
+    dev = _on_device(logits, score, done, workspace)
+    if score.dtype != torch.float32 or score.shape != (B, W) or not score.is_contiguous():
+        raise ValueError("score: contiguous fp32 [B, W]")
+    if done is not None and (done.element_size() != 1 or done.shape != (B, W) or not done.is_contiguous()):
+        raise ValueError("done: contiguous bytes [B, W]")
+    s = logits.stride()
+    ld = s[1] if W > 1 else s[0] if B > 1 else V
+    if (s[2] != 1 and V > 1) or (B * W > 1 and ld < V) or (B > 1 and s[0] != W * ld):
+        raise ValueError("logits: contiguous rows at one distance, beams within utterances")
+    stream = torch._C._cuda_getCurrentRawStream(dev)
+    arrived, scratch = _scratch_of_select(score, dev, stream, B, workspace_bytes(WS_LM_SELECT, (B, W, V)))
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    _chk(lib().q4_lm_beam_select(_p(logits), C.c_int64(max(ld, V)), C.c_int32(DTYPES[logits.dtype]), _p(score), _p(done), C.c_int32(B),
-                                 C.c_int32(W), C.c_int32(V), C.c_int32(eos), C.c_float(rho), _p(r["parent"]), _p(r["token"]),
-                                 _p(r["score"]), _p(r["done"]), _p(workspace), C.c_size_t(workspace.numel()), _stream()),
-         "q4_lm_beam_select")
-    return r
+        workspace = scratch
+    ints = score.new_empty((2, B, W), dtype=torch.int32).unbind(0)
+    out, ended = score.new_empty((B, W)), score.new_empty((B, W), dtype=torch.uint8)
+    _chk(lib().q4_lm_beam_select(logits.data_ptr(), max(ld, V), DTYPES[dtype], score.data_ptr(), _ptr(done), B, W, V, eos, rho,
+                                 ints[0].data_ptr(), ints[1].data_ptr(), out.data_ptr(), ended.data_ptr(), arrived.data_ptr(),
+                                 workspace.data_ptr(), workspace.numel(), stream), "q4_lm_beam_select")
+    return {"parent": ints[0], "token": ints[1], "score": out, "done": ended}
 
 
-def _reorder_item(t: ReorderS, src: torch.Tensor, dst: torch.Tensor, dim: int, B: int, W: int):
-    """Rows, steps and counts of a pair of tensors whose dimensions `dim` and `dim + 1` are utterance and beam."""
-    _require(src.dtype == dst.dtype and src.shape == dst.shape and src.dim() >= dim + 2 and tuple(src.shape[dim:dim + 2]) == (B, W),
-             "src and dst: alike, with utterances and beams as dimensions dim and dim + 1")
-    es, shape = src.element_size(), src.shape
-    strides = [[s * es for s in x.stride()] for x in (src, dst)]
+@functools.lru_cache(maxsize=256)
+def _reorder_layout(shape: tuple, strides: tuple, es: int, dim: int, B: int, W: int) -> tuple:
+    """Rows of a pair of tensors (strides of src and of dst in elements) whose dimensions `dim` and `dim` + 1 are utterance and
+    beam: bytes of a row, distances of rows, then counts and steps of what lies outside and inside of the beams."""
+    strides = [[s * es for s in x] for x in strides]
     for s in strides:
         _require(B < 2 or W < 2 or s[dim] == W * s[dim + 1], "rows of one utterance must follow those of the one before")
     row = [s[dim + 1] if W > 1 else s[dim] for s in strides]
-    inner = list(range(dim + 2, src.dim()))
+    inner = list(range(dim + 2, len(shape)))
     row_bytes = es
-    while inner and all(s[inner[-1]] == row_bytes or shape[inner[-1]] == 1 for s in strides):   # contiguous in both
+    while inner and (shape[inner[-1]] == 1 or all(s[inner[-1]] == row_bytes for s in strides)):   # contiguous in both
         row_bytes *= shape[inner.pop()]
 
     def one(dims):           # several dimensions that are one in both tensors, as (count, steps)
@@ -634,26 +680,34 @@ def _reorder_item(t: ReorderS, src: torch.Tensor, dst: torch.Tensor, dim: int, B
         return n, step
 
     (n0, s0), (n1, s1) = one(range(dim)), one(inner)
-    t.src, t.dst, t.row_bytes = src.data_ptr(), dst.data_ptr(), row_bytes if src.numel() else 0
-    t.src_row_step, t.dst_row_step = row
-    t.n[0], t.n[1] = n0, n1
-    t.src_step[0], t.src_step[1], t.dst_step[0], t.dst_step[1] = s0[0], s1[0], s0[1], s1[1]
+    return (row_bytes if all(shape) else 0, row[0], row[1], (n0, n1), (s0[0], s1[0]), (s0[1], s1[1]))
+
+
+def _reorder_item(t: ReorderS, src: torch.Tensor, dst: torch.Tensor, dim: int, B: int, W: int):
+    shape = src.shape
+    if src.dtype != dst.dtype or shape != dst.shape or shape[dim:dim + 2] != (B, W):
+        raise ValueError("src and dst: alike, with utterances and beams as dimensions dim and dim + 1")
+    t.src, t.dst = src.data_ptr(), dst.data_ptr()
+    t.row_bytes, t.src_row_step, t.dst_row_step, t.n[:], t.src_step[:], t.dst_step[:] = _reorder_layout(
+        shape, (src.stride(), dst.stride()), src.element_size(), dim, B, W)
 
 
 def q4_beam_reorder(pairs: Sequence, parent: torch.Tensor, dim: int = 0):
     """dst[..., b, w, ...] = src[..., b, parent[b, w], ...] for pairs (src, dst) of tensors whose dimensions `dim` and `dim` + 1
     are utterance and beam; where parent is negative dst is left as it was.  Views are fine (the used part of a cache)."""
     _need_cuda()
-    _require(parent.dim() == 2 and parent.dtype == torch.int32 and parent.is_contiguous(), "parent: contiguous int32 [B, W]")
+    if parent.dim() != 2 or parent.dtype != torch.int32 or not parent.is_contiguous():
+        raise ValueError("parent: contiguous int32 [B, W]")
+    if dim < 0:
+        raise ValueError("dim: not negative")
     B, W = parent.shape
-    _require(W > 0 or not pairs, "parent: at least one beam")
     for first in range(0, len(pairs), REORDER_MAX):
         group = pairs[first:first + REORDER_MAX]
         items = (ReorderS * len(group))()
         for item, (src, dst) in zip(items, group):
-            _on_device(parent, src, dst)
+            dev = _on_device(parent, src, dst)
             _reorder_item(item, src, dst, dim, B, W)
-        _chk(lib().q4_beam_reorder(items, C.c_int32(len(group)), _p(parent), C.c_int32(B), C.c_int32(W), _stream()),
+        _chk(lib().q4_beam_reorder(items, len(group), parent.data_ptr(), B, W, torch._C._cuda_getCurrentRawStream(dev)),
              "q4_beam_reorder")
 
 

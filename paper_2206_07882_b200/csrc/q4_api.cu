@@ -1950,16 +1950,17 @@ int q4_linear_token_scales(const void* xq, const float* x_scale, int32_t M, cons
 
 int q4_lm_beam_select(const void* logits, int64_t logits_stride, int32_t dtype, const float* score, const uint8_t* done,
                       int32_t B, int32_t W, int32_t V, int32_t eos, float rho, int32_t* parent, int32_t* token,
-                      float* score_out, uint8_t* done_out, void* workspace, size_t workspace_bytes, q4_stream stream) {
+                      float* score_out, uint8_t* done_out, uint32_t* arrived, void* workspace, size_t workspace_bytes,
+                      q4_stream stream) {
   const int es = element_bytes(dtype);
   if (!es) return Q4_ERR_UNSUPPORTED;
   if (B < 0 || W <= 0 || W > 32 || V <= 0 || logits_stride < V || (int64_t)B * W > INT32_MAX) return Q4_ERR_DIM;
   if (eos < -1 || eos >= V || (done && eos < 0) || !isfinite(rho)) return Q4_ERR_DIM;
   if (B == 0) return Q4_OK;
-  if (!logits || !score || !parent || !token || !score_out || !workspace) return Q4_ERR_NULL;
+  if (!logits || !score || !parent || !token || !score_out || !arrived || !workspace) return Q4_ERR_NULL;
   if (score_out == score || (done && done_out == done)) return Q4_ERR_UNSUPPORTED;
   if (!aligned_to(logits, es) || !aligned_to(score, 4) || !aligned_to(parent, 4) || !aligned_to(token, 4) ||
-      !aligned_to(score_out, 4) || !aligned16(workspace))
+      !aligned_to(score_out, 4) || !aligned_to(arrived, 4) || !aligned16(workspace))
     return Q4_ERR_ALIGN;
   const int32_t wd[3] = {B, W, V};
   if (workspace_bytes < q4_workspace_bytes(Q4_WS_LM_SELECT, wd, 3)) return Q4_ERR_WORKSPACE;
@@ -1979,6 +1980,7 @@ int q4_lm_beam_select(const void* logits, int64_t logits_stride, int32_t dtype, 
   a.score_out = score_out;
   a.done_out = done_out;
   a.workspace = static_cast<uint8_t*>(workspace);
+  a.arrived = arrived;
   TagScope tag(TAG_LM_SELECT);
   Q4_TRY(launch_lm_select(a, dtype, S(stream)));
   return Q4_OK;

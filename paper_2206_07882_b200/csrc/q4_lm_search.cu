@@ -25,21 +25,16 @@ template <> __device__ __forceinline__ float to_f32(__half v) { return __half2fl
 template <> __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
 
 constexpr float LOG2E = 1.4426950408889634f;
+constexpr double LOG2E_EXCESS = (double)LOG2E * 0.693147180559945309417232 - 1.0;   // of the rounded constant
 
-// A row of logits is cut into `parts` segments.  What a segment leaves for the merge: its maximum and its sum of exponentials
-// relative to it (NaN: the row holds a NaN or +inf), and its W best logits above -inf, best first, equal ones by label; label -1
-// behind the last.
-struct PartSum {
-  float top;
-  float pad;
-  double sum;
-};
+// A row of logits is cut into `parts` segments.  What a segment leaves for the merge: its log-sum-exp (-inf: nothing but -inf;
+// NaN: a NaN or +inf), and its W best logits above -inf, best first, equal ones by label; label -1 behind the last.
 struct Best {
   float value;
   int32_t label;
 };
 struct RowParts {
-  PartSum* sums;            // [B W, parts]
+  double* lse;              // [B W, parts]
   Best* best;               // [B W, parts, W]
   int32_t parts;
   int32_t vectors;          // 16-byte vectors of a segment
@@ -89,6 +84,7 @@ template <> __device__ __forceinline__ uint4 lowest_vector<__nv_bfloat16>() { re
 constexpr int ROW_NT = 256, ROW_VECTORS = 4, ROW_GROUPS = ROW_NT / 4, ROW_LIST = 512, ROW_STAGES = 3;
 constexpr int ROW_TURN = ROW_NT * ROW_VECTORS;                    // 16-byte vectors that a block reads in one turn
 constexpr int ROW_RING = ROW_STAGES * ROW_TURN * 16;              // bytes
+constexpr int MERGE_LIST = 1024;
 
 __device__ __forceinline__ void copy_async16(uint4* dst, const uint4* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
@@ -96,28 +92,87 @@ __device__ __forceinline__ void copy_async16(uint4* dst, const uint4* src) {
 __device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT> __device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
+// Sums of exponentials are kept as s 2^n, n an integer: a term is 2^(x log2 e - n), one fused multiply-add and the base-2 unit,
+// and a change of n is exact.  The rounded constant raises e to 1 + LOG2E_EXCESS, which is taken out again at the maximum.
+// n stays within 2^21: logits below that are nothing beside any above, and a segment whose maximum lies outside of +-10^6 is
+// summed in another way (`far`).
+__device__ __forceinline__ float sum_scale(float m) { return fminf(fmaxf(rintf(m * LOG2E), -2097152.0f), 2097152.0f); }
+__device__ __forceinline__ float pow2_down(float d) {   // 2^d, d <= 0 an integer; 0 below 2^-126
+  return __int_as_float((int)(fmaxf(d, -127.0f) + 127.0f) << 23);
+}
+
+// A proposal's score in double as an integer of the same order (comparisons of doubles take several times as long), and what
+// decides between equal ones.
+struct Proposal {
+  long long key;
+  float z;
+  int32_t label, beam;
+};
+constexpr long long NO_PROPOSAL = (long long)0x800fffffffffffffULL;   // the key of -inf
+__device__ __forceinline__ long long order_key(double c) {
+  const long long b = __double_as_longlong(c + 0.0);       // (-0 becomes 0)
+  return b >= 0 ? b : b ^ 0x7fffffffffffffffLL;
+}
+__device__ __forceinline__ double key_score(long long k) { return __longlong_as_double(k >= 0 ? k : k ^ 0x7fffffffffffffffLL); }
+__device__ __forceinline__ bool before(const Proposal& a, const Proposal& b) {
+  return a.key > b.key || (a.key == b.key && (a.beam < b.beam || (a.beam == b.beam && before(a.z, a.label, b.z, b.label))));
+}
+
+struct SelectShared {
+  float value[ROW_LIST];
+  int32_t label[ROW_LIST], vector[ROW_LIST];
+  Best best[64];
+  double sum[ROW_NT / 32];
+  float group[ROW_GROUPS], top[ROW_NT / 32], scale[ROW_NT / 32];
+  int32_t vectors, n, some, last;
+};
+// What the merge needs lies where the copies landed (a block's last turn has been waited for by then)
+struct MergeShared {
+  double score[MAX_BEAMS], lse[MAX_BEAMS];   // lse NaN: the beam proposes nothing
+  int32_t ended[MAX_BEAMS];
+  long long key[MERGE_LIST];
+  float z[MERGE_LIST];
+  int32_t label[MERGE_LIST], beam[MERGE_LIST];
+};
+static_assert(sizeof(MergeShared) <= (size_t)ROW_RING && MERGE_LIST >= ROW_NT, "the merge's shared memory");
+
+// The W-th largest of the block's ROW_GROUPS group maxima, at least (W of the elements are no smaller): every thread of the first
+// two warps counts what is larger than its own, and the smallest of those with fewer than W larger ones is taken.
+__device__ __forceinline__ float group_bound(SelectShared& sh, float mine, int W) {
+  mine = fmaxf(mine, __shfl_xor_sync(0xffffffffu, mine, 1));
+  mine = fmaxf(mine, __shfl_xor_sync(0xffffffffu, mine, 2));
+  const int tid = threadIdx.x;
+  if ((tid & 3) == 0) sh.group[tid >> 2] = mine;
+  __syncthreads();
+  if (tid < ROW_GROUPS) {
+    mine = sh.group[tid];
+    int larger = 0;
+#pragma unroll
+    for (int i = 0; i < ROW_GROUPS; i += 4) {
+      const float4 o = *reinterpret_cast<const float4*>(sh.group + i);
+      larger += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
+    }
+    float low = larger < W ? mine : INFINITY;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) low = fminf(low, __shfl_xor_sync(0xffffffffu, low, o));
+    if ((tid & 31) == 0) sh.top[tid >> 5] = low;
+  }
+  __syncthreads();
+  return fminf(sh.top[0], sh.top[1]);
+}
+
 // One pass over a segment: running maximum and sum of every thread, and the candidates for the segment's W best.
-// A bound on those comes from the first turn: the W-th best of the maxima of 64 groups of four threads.  W of its elements are
-// no smaller, so of the elements behind it only larger ones count (equal ones come later in the order).  About 20 (W = 16) to
-// 45 (W = 32) elements of a turn pass a bound like that; they are ranked at the end.  A list that overflows (equal or rising
-// logits) is given up for W passes over the segment.
+// A bound on those comes from the first turn (group_bound): of the elements behind it only larger ones count (equal ones come
+// later in the order).  About 18 (W = 16) to 45 (W = 32) elements of a turn pass a bound like that.  The loop notes the vectors
+// that hold them; their elements are looked at again and ranked at the end.  A list that overflows (equal or rising logits) is
+// given up for W passes over the segment.
 // Every thread copies the vectors it will read itself into shared memory, two turns ahead: no barrier in the loop, no registers
 // for what is on its way, and four blocks of an SM keep 128 KB in flight.
 template <typename T>
-__global__ void __launch_bounds__(ROW_NT, 4) k_lm_rows(const LmSelectArgs a, const RowParts p) {
+__device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const RowParts& p, long long row, int part, SelectShared& sh,
+                                                uint4* ring) {
   constexpr int N = Vec<T>::N;
-  extern __shared__ uint4 s_ring[];
-  __shared__ __align__(16) Best s_list[ROW_LIST];
-  __shared__ __align__(16) float s_group[ROW_GROUPS];
-  __shared__ float s_top[ROW_NT / 32];
-  __shared__ double s_sum[ROW_NT / 32];
-  __shared__ float s_bound;
-  __shared__ int s_n;
-  const long long row = blockIdx.x / p.parts;
-  const int part = blockIdx.x % p.parts, tid = threadIdx.x, W = a.W;
-  pdl_wait();
-  pdl_trigger();   // the merge waits for this grid's end before it reads anything
-  if (!isfinite(a.score[row]) || (a.done && a.done[row])) return;   // the merge does not look at the row
+  const int tid = threadIdx.x, W = a.W;
   const T* z = static_cast<const T*>(a.logits) + row * a.ld;
   // elements in front of the first 16-byte boundary, vectors, and elements behind the last whole vector
   const int head = min((int)(((16 - (reinterpret_cast<uintptr_t>(z) & 15)) & 15) / sizeof(T)), a.V);
@@ -125,134 +180,190 @@ __global__ void __launch_bounds__(ROW_NT, 4) k_lm_rows(const LmSelectArgs a, con
   const uint4* body = reinterpret_cast<const uint4*>(z + head);
   const int v0 = min(part * p.vectors, n_vec), v1 = part + 1 == p.parts ? n_vec : min(v0 + p.vectors, n_vec);
   const int turns = max((v1 - v0 + ROW_TURN - 1) / ROW_TURN, 1);
-  auto fetch = [&](int t) {
-    if (t < turns) {
-      uint4* slot = s_ring + (t % ROW_STAGES) * ROW_TURN + tid;
+  const uint4* src = body + v0 + tid;              // first vector of the next turn to fetch
+  int left = v1 - v0 - tid, to_slot = tid;         // vectors from there on; its place in the ring
+  auto fetch = [&]() {
+    uint4* slot = ring + to_slot;
+    if (left > (ROW_VECTORS - 1) * ROW_NT) {
 #pragma unroll
-      for (int j = 0; j < ROW_VECTORS; ++j) {
-        const int v = v0 + t * ROW_TURN + j * ROW_NT + tid;
-        if (v < v1) copy_async16(slot + j * ROW_NT, body + v);
-      }
+      for (int j = 0; j < ROW_VECTORS; ++j) copy_async16(slot + j * ROW_NT, src + j * ROW_NT);
+    } else {
+#pragma unroll
+      for (int j = 0; j < ROW_VECTORS; ++j)
+        if (j * ROW_NT < left)
+          copy_async16(slot + j * ROW_NT, src + j * ROW_NT);
+        else
+          slot[j * ROW_NT] = lowest_vector<T>();
     }
     copy_async_commit();
+    src += ROW_TURN;
+    left -= ROW_TURN;
+    to_slot = to_slot < (ROW_STAGES - 1) * ROW_TURN ? to_slot + ROW_TURN : tid;
   };
 #pragma unroll
-  for (int t = 0; t < ROW_STAGES - 1; ++t) fetch(t);
+  for (int t = 0; t < ROW_STAGES - 1; ++t) fetch();
   const int tail = head + n_vec * N;
   int extra_at = -1;
   if (part == 0 && tid < head) extra_at = tid;
   if (part + 1 == p.parts && tid >= 32 && tid < 32 + a.V - tail) extra_at = tail + tid - 32;
   const float extra = extra_at >= 0 ? to_f32<T>(z[extra_at]) : -INFINITY;
-  if (tid == 0) s_n = 0;
+  if (tid == 0) sh.vectors = sh.n = sh.some = 0;
 
-  float m = extra != extra ? -INFINITY : extra, bound = 0.0f;
-  float sum = extra == -INFINITY ? 0.0f : extra < INFINITY ? 1.0f : NAN;   // a NaN or +inf makes the row's sum NaN
+  float m = extra != extra ? -INFINITY : extra, scale = sum_scale(m), bound = 0.0f, limit = 0.0f;
+  float sum = exp2_unit(__fmaf_rn(extra, LOG2E, -scale));   // (a NaN makes the sum NaN)
+  int from_slot = tid;
   for (int t = 0; t < turns; ++t) {
     copy_async_wait<ROW_STAGES - 2>();
-    const uint4* slot = s_ring + (t % ROW_STAGES) * ROW_TURN + tid;
-    const int left = v1 - (v0 + t * ROW_TURN + tid);              // vectors from this thread's first one to the end
-    auto vector = [&](int j, float (&x)[N]) { Vec<T>::get(j * ROW_NT < left ? slot[j * ROW_NT] : lowest_vector<T>(), x); };
-    float top = -INFINITY;
+    const uint4* slot = ring + from_slot;
+    from_slot = from_slot < (ROW_STAGES - 1) * ROW_TURN ? from_slot + ROW_TURN : tid;
+    float vector_top[ROW_VECTORS], top = -INFINITY;
 #pragma unroll
     for (int j = 0; j < ROW_VECTORS; ++j) {
       float x[N];
-      vector(j, x);
+      Vec<T>::get(slot[j * ROW_NT], x);
+      vector_top[j] = x[0];
 #pragma unroll
-      for (int i = 0; i < N; ++i) top = fmaxf(top, x[i]);
+      for (int i = 1; i < N; ++i) vector_top[j] = fmaxf(vector_top[j], x[i]);
+      top = fmaxf(top, vector_top[j]);
     }
-    fetch(t + ROW_STAGES - 1);
+    fetch();
     if (t == 0) {
-      float g = fmaxf(top, m);
-      g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 1));
-      g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 2));
-      if ((tid & 3) == 0) s_group[tid >> 2] = g;
-      __syncthreads();
-      if (tid < ROW_GROUPS) {
-        const float mine = s_group[tid];
-        int rank = 0;
+      bound = group_bound(sh, fmaxf(top, m), W);
+      limit = nextafterf(bound, -INFINITY);   // the first turn's elements count from the bound on
+      if (extra > limit) {
+        const int at = atomicAdd(&sh.n, 1);   // (there are at most 14 of these)
+        sh.value[at] = extra;
+        sh.label[at] = extra_at;
+      }
+    }
+    if (top > limit) {
 #pragma unroll
-        for (int i = 0; i < ROW_GROUPS; i += 4) {
-          const float4 o = *reinterpret_cast<const float4*>(s_group + i);
-          rank += (o.x > mine || (o.x == mine && i < tid)) + (o.y > mine || (o.y == mine && i + 1 < tid)) +
-                  (o.z > mine || (o.z == mine && i + 2 < tid)) + (o.w > mine || (o.w == mine && i + 3 < tid));
+      for (int j = 0; j < ROW_VECTORS; ++j)
+        if (vector_top[j] > limit) {
+          const int at = atomicAdd(&sh.vectors, 1);
+          if (at < ROW_LIST) sh.vector[at] = v0 + t * ROW_TURN + j * ROW_NT + tid;
         }
-        if (rank == W - 1) s_bound = mine;
-      }
-      __syncthreads();
-      bound = s_bound;
-      if (extra > -INFINITY && extra >= bound) {
-        const int at = atomicAdd(&s_n, 1);
-        if (at < ROW_LIST) s_list[at] = Best{extra, extra_at};
-      }
     }
-    // (elements of the first turn count from the bound on, later ones above it only)
-    if (t == 0 ? top >= bound && top > -INFINITY : top > bound) {
-#pragma unroll
-      for (int j = 0; j < ROW_VECTORS; ++j) {
-        float x[N];
-        vector(j, x);
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-          if (t == 0 ? x[i] >= bound && x[i] > -INFINITY : x[i] > bound) {
-            const int at = atomicAdd(&s_n, 1);
-            if (at < ROW_LIST) s_list[at] = Best{x[i], head + (v0 + t * ROW_TURN + j * ROW_NT + tid) * N + i};
-          }
-      }
-    }
-    const float next_m = fmaxf(m, top), base = next_m > -INFINITY ? next_m : 0.0f;
-    float part_sum[2] = {0.0f, 0.0f};
+    limit = bound;
+    m = fmaxf(m, top);
+    const float next = sum_scale(m);
+    const uint64_t mul = pk2(LOG2E, LOG2E), sub = pk2(-next, -next);
+    uint64_t part_sum = pk2(0.0f, 0.0f);
 #pragma unroll
     for (int j = 0; j < ROW_VECTORS; ++j) {
       float x[N];
-      vector(j, x);
+      Vec<T>::get(slot[j * ROW_NT], x);
 #pragma unroll
-      for (int i = 0; i < N; ++i) part_sum[i & 1] += exp2_unit((x[i] - base) * LOG2E);
+      for (int i = 0; i < N; i += 2) {
+        float e0, e1;
+        upk2(fma2(pk2(x[i], x[i + 1]), mul, sub), e0, e1);
+        part_sum = add2(part_sum, pk2(exp2_unit(e0), exp2_unit(e1)));
+      }
     }
-    sum = sum * exp2_unit((m - base) * LOG2E) + (part_sum[0] + part_sum[1]);
-    m = next_m;
+    float even, odd;
+    upk2(part_sum, even, odd);
+    sum = sum * pow2_down(scale - next) + (even + odd);
+    scale = next;
   }
 
-  float top = m;
+  float top = m, most = scale;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  if ((tid & 31) == 0) s_top[tid >> 5] = top;
+  for (int o = 16; o > 0; o >>= 1) {
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+  }
+  __syncthreads();                             // (the bound has been read)
+  if ((tid & 31) == 0) {
+    sh.top[tid >> 5] = top;
+    sh.scale[tid >> 5] = most;
+  }
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < ROW_NT / 32; ++w) top = fmaxf(top, s_top[w]);
-  double total = (double)(sum * exp2_unit((m - (top > -INFINITY ? top : 0.0f)) * LOG2E));
+  for (int w = 0; w < ROW_NT / 32; ++w) {
+    top = fmaxf(top, sh.top[w]);
+    most = fmaxf(most, sh.scale[w]);
+  }
+  const int n_vectors = sh.vectors;
+  const bool far = top > -INFINITY && fabsf(top) > 1e6f;
+  double total = (double)(sum * pow2_down(scale - most));
+  const int from = part == 0 ? 0 : head + v0 * N, to = part + 1 == p.parts ? a.V : head + v1 * N;
+  if (far) {   // differences from the maximum, which are exact where they count
+    total = 0.0;
+    for (int k = from + tid; k < to; k += ROW_NT) total += (double)exp2_unit((to_f32<T>(z[k]) - top) * LOG2E);
+  }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-  if ((tid & 31) == 0) s_sum[tid >> 5] = total;
+  if ((tid & 31) == 0) sh.sum[tid >> 5] = total;
+  // elements of the noted vectors
+  for (int i = tid; i < min(n_vectors, ROW_LIST); i += ROW_NT) {
+    const int v = sh.vector[i];
+    float x[N];
+    Vec<T>::get(turns <= ROW_STAGES ? ring[v - v0] : __ldg(body + v), x);   // (the ring still holds a short segment)
+    limit = v < v0 + ROW_TURN ? nextafterf(bound, -INFINITY) : bound;
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (x[j] > limit) {
+        const int at = atomicAdd(&sh.n, 1);
+        if (at < ROW_LIST) {
+          sh.value[at] = x[j];
+          sh.label[at] = head + v * N + j;
+        }
+      }
+  }
   __syncthreads();
   const long long out = row * p.parts + part;
-  if (tid == 0) {
+  if (tid == ROW_NT - 1) {   // (a warp that has the least to rank)
     total = 0.0;
 #pragma unroll
-    for (int w = 0; w < ROW_NT / 32; ++w) total += s_sum[w];
-    p.sums[out] = PartSum{top, 0.0f, total};
+    for (int w = 0; w < ROW_NT / 32; ++w) total += sh.sum[w];
+    const double excess = far ? 0.0 : LOG2E_EXCESS * (double)top, base = far ? (double)top : (double)most * 0.693147180559945309417232;
+    p.lse[out] = top == -INFINITY ? (total == 0.0 ? -INFINITY : NAN) : base + log(total) - excess;
   }
   Best* best = p.best + out * W;
-  const int n = s_n;
-  if (n <= ROW_LIST) {
-    constexpr int UNROLL = 8;
-    const int n_pad = (n + UNROLL - 1) / UNROLL * UNROLL;   // (ROW_LIST is a multiple)
-    if (n + tid < n_pad) s_list[n + tid] = Best{-INFINITY, INT32_MAX};
+  int n = sh.n;
+  if (n_vectors <= ROW_LIST && n <= ROW_LIST) {
+    // those with fewer than W larger ones, W and what is equal to the last of them, into a short list; their places in that
+    if (n + tid < (n + 3) / 4 * 4) sh.value[n + tid] = -INFINITY;
     __syncthreads();
-    for (int i = tid; i < max(n, W); i += ROW_NT) {
-      if (i >= n) {
-        best[i] = Best{-INFINITY, -1};
-        continue;
+    for (int i = tid; i < n; i += ROW_NT) {
+      const float mine = sh.value[i];
+      int larger = 0;
+#pragma unroll 4
+      for (int j = 0; j < n; j += 4) {
+        const float4 o = *reinterpret_cast<const float4*>(sh.value + j);
+        larger += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
       }
-      const Best mine = s_list[i];
-      int rank = 0;
-      for (int j = 0; j < n_pad; j += UNROLL)
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) rank += before(s_list[j + u].value, s_list[j + u].label, mine.value, mine.label);
-      if (rank < W) best[rank] = mine;
+      if (larger < W) {
+        const int at = atomicAdd(&sh.some, 1);
+        if (at < 64) sh.best[at] = Best{mine, sh.label[i]};
+      }
     }
-    return;
+    __syncthreads();
+    n = sh.some;
+    if (n <= 64) {
+      if (tid < max(n, W)) {
+        if (tid >= n) {
+          best[tid] = Best{-INFINITY, -1};
+        } else {
+          const Best mine = sh.best[tid];
+          int rank = 0;
+#pragma unroll 4
+          for (int j = 0; j < n; ++j) rank += before(sh.best[j].value, sh.best[j].label, mine.value, mine.label);
+          if (rank < W) best[rank] = mine;
+        }
+      }
+      return;
+    }
+    n = sh.n;
+    for (int i = tid; i < n; i += ROW_NT) {   // many equal ones
+      const float mine = sh.value[i];
+      const int label = sh.label[i];
+      int rank = 0;
+      for (int j = 0; j < n; ++j) rank += before(sh.value[j], sh.label[j], mine, label);
+      if (rank < W) best[rank] = Best{mine, label};
+    }
+    return;                                    // (more than 64 elements, so W of them)
   }
-  const int from = part == 0 ? 0 : head + v0 * N, to = part + 1 == p.parts ? a.V : head + v1 * N;
   Best last{INFINITY, -1};
   for (int i = 0; i < W; ++i) {
     Best b{-INFINITY, INT32_MAX};
@@ -266,151 +377,163 @@ __global__ void __launch_bounds__(ROW_NT, 4) k_lm_rows(const LmSelectArgs a, con
       if (before(c.value, c.label, b.value, b.label)) b = c;
     }
     __syncthreads();
-    if ((tid & 31) == 0) s_list[tid >> 5] = b;
+    if ((tid & 31) == 0) sh.best[tid >> 5] = b;
     __syncthreads();
     for (int w = 0; w < ROW_NT / 32; ++w)
-      if (before(s_list[w].value, s_list[w].label, b.value, b.label)) b = s_list[w];
+      if (before(sh.best[w].value, sh.best[w].label, b.value, b.label)) b = sh.best[w];
     if (tid == 0) best[i] = b.label == INT32_MAX ? Best{-INFINITY, -1} : b;   // (overflowed: there are more than W)
     last = b;
   }
 }
 
-// One block per utterance.  A proposal's score is score[w] + (z - lse + rho) in double; lse from the segments' sums.
-// As in k_lm_rows the W-th best of the maxima of 128 groups (rounded down to fp32, so it errs on the safe side) bounds the W best
-// from below, and the proposals that reach it are ranked.  Every entry of the lists has a thread of its own where there are enough: a
-// walk down the lists took 20 us in dependent loads.
-struct Proposal {
-  double c;
-  float z;
-  int32_t label, beam;
-};
-__device__ __forceinline__ bool before(const Proposal& a, const Proposal& b) {
-  return a.c > b.c || (a.c == b.c && (a.beam < b.beam || (a.beam == b.beam && before(a.z, a.label, b.z, b.label))));
-}
-constexpr int MERGE_NT = 512, MERGE_GROUPS = 128, MERGE_LIST = 512;
-
-__global__ void __launch_bounds__(MERGE_NT) k_lm_merge(const LmSelectArgs a, const RowParts p) {
-  __shared__ double s_score[MAX_BEAMS], s_lse[MAX_BEAMS];   // lse NaN: the beam proposes nothing
-  __shared__ int s_ended[MAX_BEAMS];
-  __shared__ __align__(16) float s_group[MERGE_GROUPS];
-  __shared__ Proposal s_list[MERGE_LIST];
-  __shared__ float s_bound;
-  __shared__ int s_n;
+// The W best proposals of an utterance from its segments' lists.  A proposal's score is score[w] + (z - lse + rho) in double; the
+// segments' shares of lse are put together first.  As for a segment a bound from group maxima (rounded down to fp32, so it errs
+// on the safe side) leaves few proposals to rank.  Every entry of the lists has a thread of its own where there are enough: a walk
+// down the lists took 20 us in dependent loads.
+__device__ __forceinline__ void merge_segments(const LmSelectArgs& a, const RowParts& p, int utterance, SelectShared& sh, MergeShared& mg) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, W = a.W;
-  const long long row0 = (long long)blockIdx.x * W;
-  if (tid == 0) s_n = 0;
-  pdl_wait();
-  // entries of all lists of the utterance, entry ((w parts + i) W + j): place j of segment i of beam w
+  const long long row0 = (long long)utterance * W;
+  // entry ((w parts + i) W + j): place j of segment i of beam w
   const int per_beam = p.parts * W, entries = W * per_beam;
   const Best* all = p.best + row0 * per_beam;
-  const Best first = tid < entries ? all[tid] : Best{};     // on its way while the sums are put together
-  for (int w = warp; w < W; w += MERGE_NT / 32) {
-    const float score = a.score[row0 + w];
-    const bool ended = isfinite(score) && a.done && a.done[row0 + w];
-    double lse = NAN;
-    if (isfinite(score) && !ended) {
-      const PartSum* ps = p.sums + (row0 + w) * p.parts;
-      PartSum mine = lane < p.parts ? ps[lane] : PartSum{-INFINITY, 0.0f, 0.0};
-      float top = mine.top;
-      for (int i = lane + 32; i < p.parts; i += 32) top = fmaxf(top, ps[i].top);
+  auto entry = [&](int e) {   // past the L1: other blocks wrote it
+    const int2 v = __ldcg(reinterpret_cast<const int2*>(all) + e);
+    return Best{__int_as_float(v.x), v.y};
+  };
+  const Best first = tid < entries ? entry(tid) : Best{-INFINITY, -1};     // on its way while the sums are put together
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      if (top > -INFINITY && top < INFINITY) {
-        double sum = mine.sum * (double)exp2_unit((mine.top - top) * LOG2E);
-        for (int i = lane + 32; i < p.parts; i += 32) sum += ps[i].sum * (double)exp2_unit((ps[i].top - top) * LOG2E);
-        for (int o = 16; o > 0; o >>= 1)
-          if (o < p.parts) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        lse = (double)top + log(sum);
+  for (int i = 0; i < MAX_BEAMS / (ROW_NT / 32); ++i) {
+    const int w = warp + i * (ROW_NT / 32);
+    if (w >= W) break;
+    const double* parts = p.lse + (row0 + w) * p.parts;
+    const float score = a.score[row0 + w];
+    const bool ended = a.done && a.done[row0 + w] && isfinite(score);
+    double lse = lane < p.parts ? __ldcg(parts + lane) : -INFINITY;         // (a beam that is empty or ended left none: not used)
+    if (p.parts > 1 && isfinite(score) && !ended) {
+      double top = lse;
+      bool bad = isnan(lse);
+      for (int j = lane + 32; j < p.parts; j += 32) {
+        top = fmax(top, __ldcg(parts + j));
+        bad = bad || isnan(__ldcg(parts + j));
       }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) top = fmax(top, __shfl_xor_sync(0xffffffffu, top, o));
+      double sum = (double)exp2_unit((float)(lse - top) * LOG2E);
+      for (int j = lane + 32; j < p.parts; j += 32) sum += (double)exp2_unit((float)(__ldcg(parts + j) - top) * LOG2E);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      lse = __any_sync(0xffffffffu, bad) ? NAN : top + log(sum);
     }
     if (lane == 0) {
-      s_score[w] = score;
-      s_lse[w] = lse;
-      s_ended[w] = ended;
+      mg.score[w] = score;
+      mg.lse[w] = isfinite(score) && !ended && isfinite(lse) ? lse : NAN;   // (not finite: nothing but -inf, a NaN or +inf)
+      mg.ended[w] = ended;
     }
   }
+  if (tid == 0) sh.n = 0;
   __syncthreads();
   auto proposal = [&](int e, const Best& b) {
     const int w = e / per_beam;
-    Proposal q{-INFINITY, -INFINITY, -1, w};
-    if (s_ended[w]) {
-      if (e == w * per_beam) q.c = s_score[w], q.z = 0.0f, q.label = a.eos;
-    } else if (!isnan(s_lse[w]) && b.label >= 0) {
-      q.c = s_score[w] + (((double)b.value - s_lse[w]) + (double)a.rho);
-      q.z = b.value;
-      q.label = b.label;
-      if (!isfinite((float)q.c)) q.c = -INFINITY;
+    Proposal q{NO_PROPOSAL, -INFINITY, -1, w};
+    if (mg.ended[w]) {
+      if (e == w * per_beam) q = Proposal{order_key(mg.score[w]), 0.0f, a.eos, w};
+    } else if (!isnan(mg.lse[w]) && b.label >= 0) {
+      const double c = mg.score[w] + (((double)b.value - mg.lse[w]) + (double)a.rho);
+      if (isfinite((float)c)) q = Proposal{order_key(c), b.value, b.label, w};
     }
     return q;
   };
-  Proposal mine{-INFINITY, -INFINITY, -1, 0};
+  Proposal mine{NO_PROPOSAL, -INFINITY, -1, 0};
   if (tid < entries) mine = proposal(tid, first);
-  float head = __double2float_rd(mine.c);
-  for (int e = tid + MERGE_NT; e < entries; e += MERGE_NT) head = fmaxf(head, __double2float_rd(proposal(e, all[e]).c));
-#pragma unroll
-  for (int o = 1; o < MERGE_NT / MERGE_GROUPS; o <<= 1) head = fmaxf(head, __shfl_xor_sync(0xffffffffu, head, o));
-  if (tid % (MERGE_NT / MERGE_GROUPS) == 0) s_group[tid / (MERGE_NT / MERGE_GROUPS)] = head;
-  __syncthreads();
-  if (tid < MERGE_GROUPS) {
-    const float g = s_group[tid];
-    int rank = 0;
-#pragma unroll
-    for (int i = 0; i < MERGE_GROUPS; i += 4) {
-      const float4 o = *reinterpret_cast<const float4*>(s_group + i);
-      rank += (o.x > g || (o.x == g && i < tid)) + (o.y > g || (o.y == g && i + 1 < tid)) + (o.z > g || (o.z == g && i + 2 < tid)) +
-              (o.w > g || (o.w == g && i + 3 < tid));
-    }
-    if (rank == W - 1) s_bound = g;
-  }
-  __syncthreads();
-  const double bound = s_bound;
+  long long head = mine.key;
+  for (int e = tid + ROW_NT; e < entries; e += ROW_NT) head = max(head, proposal(e, entry(e)).key);
+  const float low = group_bound(sh, __double2float_rd(key_score(head)), W);
+  const long long bound = order_key((double)low);
   auto offer = [&](const Proposal& q) {
-    if (q.c > -INFINITY && q.c >= bound) {
-      const int at = atomicAdd(&s_n, 1);
-      if (at < MERGE_LIST) s_list[at] = q;
+    if (q.key > NO_PROPOSAL && q.key >= bound) {
+      const int at = atomicAdd(&sh.n, 1);
+      if (at < MERGE_LIST) {
+        mg.key[at] = q.key;
+        mg.z[at] = q.z;
+        mg.label[at] = q.label;
+        mg.beam[at] = q.beam;
+      }
     }
   };
   offer(mine);
-  for (int e = tid + MERGE_NT; e < entries; e += MERGE_NT) offer(proposal(e, all[e]));
+  for (int e = tid + ROW_NT; e < entries; e += ROW_NT) offer(proposal(e, entry(e)));
   __syncthreads();
-  const int n = s_n;
+  const int n = sh.n;
   auto store = [&](int i, const Proposal& q, bool some) {
     const long long o = row0 + i;
     a.parent[o] = some ? q.beam : -1;
     a.token[o] = some ? q.label : -1;
-    a.score_out[o] = some ? (float)q.c : -INFINITY;
+    a.score_out[o] = some ? (float)key_score(q.key) : -INFINITY;
     if (a.done_out) a.done_out[o] = some && q.label == a.eos;
   };
+  auto listed = [&](int i) { return Proposal{mg.key[i], mg.z[i], mg.label[i], mg.beam[i]}; };
   if (n <= MERGE_LIST) {
-    for (int i = tid; i < max(n, W); i += MERGE_NT) {
+    for (int i = tid; i < max(n, W); i += ROW_NT) {
       if (i >= n) {
         store(i, Proposal{}, false);
         continue;
       }
-      const Proposal q = s_list[i];
-      int rank = 0;
-#pragma unroll 4
-      for (int j = 0; j < n; ++j) rank += before(s_list[j], q);
+      const Proposal q = listed(i);
+      int rank = 0, equal = 0;
+#pragma unroll 8
+      for (int j = 0; j < n; ++j) {
+        const long long k = mg.key[j];
+        rank += k > q.key;
+        equal += k == q.key;
+      }
+      if (rank < W && equal > 1)
+        for (int j = 0; j < n; ++j) rank += mg.key[j] == q.key && before(listed(j), q);
       if (rank < W) store(rank, q, true);
     }
     return;
   }
   // more proposals at the bound than the list holds (equal beams of equal logits): one after the other
-  Proposal last{INFINITY, INFINITY, -1, -1};
+  Proposal last{INT64_MAX, INFINITY, -1, -1};
   for (int i = 0; i < W; ++i) {
-    Proposal b{-INFINITY, -INFINITY, INT32_MAX, INT32_MAX};
-    for (int e = tid; e < entries; e += MERGE_NT) {
-      const Proposal q = proposal(e, all[e]);
-      if (q.c > -INFINITY && before(last, q) && before(q, b)) b = q;
+    Proposal b{NO_PROPOSAL, -INFINITY, INT32_MAX, INT32_MAX};
+    for (int e = tid; e < entries; e += ROW_NT) {
+      const Proposal q = proposal(e, entry(e));
+      if (q.key > NO_PROPOSAL && before(last, q) && before(q, b)) b = q;
     }
     __syncthreads();
-    s_list[tid] = b;
+    mg.key[tid] = b.key;
+    mg.z[tid] = b.z;
+    mg.label[tid] = b.label;
+    mg.beam[tid] = b.beam;
     __syncthreads();
-    for (int j = 0; j < MERGE_NT; ++j)
-      if (before(s_list[j], b)) b = s_list[j];
+    for (int j = 0; j < ROW_NT; ++j)
+      if (before(listed(j), b)) b = listed(j);
     if (tid == 0) store(i, b, true);                        // (overflowed: there are more than W)
     last = b;
   }
+}
+
+// One block per segment; the last block of an utterance to be through its segment merges them all.  A block that arrives publishes
+// what its threads wrote (a barrier and a fence before the count), the last one reads the others' after the count and a fence, past
+// the L1.  The count wraps to 0 for the next call.
+template <typename T>
+__global__ void __launch_bounds__(ROW_NT, 4) k_lm_select(const LmSelectArgs a, const RowParts p) {
+  extern __shared__ uint4 s_ring[];
+  __shared__ __align__(16) SelectShared sh;
+  const long long row = blockIdx.x / p.parts;
+  const int part = blockIdx.x % p.parts, utterance = (int)(row / a.W);
+  pdl_wait();
+  pdl_trigger();   // (nothing of a later kernel starts to read or write before this grid has ended)
+  if (isfinite(a.score[row]) && !(a.done && a.done[row])) best_of_segment<T>(a, p, row, part, sh, s_ring);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const uint32_t blocks = (uint32_t)a.W * p.parts;
+    __threadfence();
+    sh.last = atomicInc(a.arrived + utterance, blocks - 1) == blocks - 1;
+    __threadfence();
+  }
+  __syncthreads();
+  if (sh.last) merge_segments(a, p, utterance, sh, *reinterpret_cast<MergeShared*>(s_ring));
 }
 
 // Moves of up to Q4_REORDER_MAX tensors, cut into vectors of `width` bytes.
@@ -461,7 +584,7 @@ __global__ void __launch_bounds__(256) k_beam_reorder(const __grid_constant__ Mo
 
 }  // namespace
 
-// Segments of a row: at least as many as keep their lists short (8 bounds of 4096 elements, see k_lm_rows), and more while there
+// Segments of a row: at least as many as keep their lists short (8 bounds of 4096 elements, see k_lm_select), and more while there
 // are fewer than 4 blocks per SM and segments of more than one such bound; they are as long as one another.
 static RowParts row_parts(int B, int W, int V, int bytes, uint8_t* workspace) {
   const long long rows = (long long)B * W;
@@ -475,8 +598,8 @@ static RowParts row_parts(int B, int W, int V, int bytes, uint8_t* workspace) {
   p.parts = (int)parts;
   const long long vectors = (V * (long long)bytes + 15) / 16;
   p.vectors = (int)((vectors + parts - 1) / parts);
-  p.sums = reinterpret_cast<PartSum*>(workspace);
-  p.best = reinterpret_cast<Best*>(workspace + align_up((size_t)rows * parts * sizeof(PartSum)));
+  p.lse = reinterpret_cast<double*>(workspace);
+  p.best = reinterpret_cast<Best*>(workspace + align_up((size_t)rows * parts * sizeof(double)));
   return p;
 }
 
@@ -484,34 +607,32 @@ size_t lm_select_workspace(int B, int W, int V) {
   size_t n = 0;
   for (int bytes = 2; bytes <= 4; bytes += 2) {
     const size_t parts = (size_t)row_parts(B > 0 ? B : 1, W, V, bytes, nullptr).parts, rows = (size_t)B * W;
-    const size_t need = align_up(rows * parts * sizeof(PartSum)) + align_up(rows * parts * W * sizeof(Best));
+    const size_t need = align_up(rows * parts * sizeof(double)) + align_up(rows * parts * W * sizeof(Best));
     n = need > n ? need : n;
   }
   return n;
 }
 
 template <typename T>
-static cudaError_t launch_rows(const LmSelectArgs& a, const RowParts& p, cudaStream_t s) {
+static cudaError_t launch_select(const LmSelectArgs& a, const RowParts& p, cudaStream_t s) {
   static bool configured_on[MAX_DEVICES];
   bool& configured = configured_on[device_slot()];
   if (!configured) {
-    const cudaError_t e = cudaFuncSetAttribute(k_lm_rows<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, ROW_RING);
+    const cudaError_t e = cudaFuncSetAttribute(k_lm_select<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, ROW_RING);
     if (e != cudaSuccess) return e;
     configured = true;
   }
-  return launch_ex(k_lm_rows<T>, dim3((unsigned)((long long)a.B * a.W * p.parts)), dim3(ROW_NT), ROW_RING, s, true, 1, a, p);
+  return launch_ex(k_lm_select<T>, dim3((unsigned)((long long)a.B * a.W * p.parts)), dim3(ROW_NT), ROW_RING, s, true, 1, a, p);
 }
 cudaError_t launch_lm_select(const LmSelectArgs& a, int dtype, cudaStream_t s) {
   const RowParts p = row_parts(a.B, a.W, a.V, dtype == Q4_F32 ? 4 : 2, a.workspace);
   if ((long long)a.B * a.W * p.parts > 0x7fffffffLL) return cudaErrorInvalidValue;
   timing_begin(s);
-  cudaError_t e = dtype == Q4_F32 ? launch_rows<float>(a, p, s) : dtype == Q4_F16 ? launch_rows<__half>(a, p, s) : launch_rows<__nv_bfloat16>(a, p, s);
+  const cudaError_t e = dtype == Q4_F32   ? launch_select<float>(a, p, s)
+                        : dtype == Q4_F16 ? launch_select<__half>(a, p, s)
+                                          : launch_select<__nv_bfloat16>(a, p, s);
   timing_end(s);
-  if (e != cudaSuccess) return e;
-  timing_begin(s);
-  e = launch_ex(k_lm_merge, dim3((unsigned)a.B), dim3(MERGE_NT), 0, s, true, 1, a, p);
-  timing_end(s);
-  g_launches += 2;
+  ++g_launches;
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 

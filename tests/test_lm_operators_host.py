@@ -51,18 +51,18 @@ def test_linear_refusals(Bd):
 
 
 def test_select_refusals_and_workspace(Bd):
-    def call(z=FAKE, ld=100, dtype=0, score=FAKE, done=None, B=2, W=4, V=100, eos=-1, rho=0.0, par=P(8192), tok=P(8192), so=P(8192), do=None,
+    def call(z=FAKE, ld=100, dtype=0, score=FAKE, done=None, B=2, W=4, V=100, eos=-1, rho=0.0, par=P(8192), tok=P(8192), so=P(8192), do=None, arr=FAKE,
              ws=FAKE, n=1 << 30):
         return Bd.lib().q4_lm_beam_select(z, C.c_int64(ld), C.c_int32(dtype), score, done, C.c_int32(B), C.c_int32(W), C.c_int32(V),
-                                          C.c_int32(eos), C.c_float(rho), par, tok, so, do, ws, C.c_size_t(n), None)
+                                          C.c_int32(eos), C.c_float(rho), par, tok, so, do, arr, ws, C.c_size_t(n), None)
     assert call(dtype=-1) == -6
     assert call(B=-1) == -2 and call(W=0) == -2 and call(W=33) == -2 and call(V=0) == -2 and call(ld=99) == -2
     assert call(B=1 << 30, W=4) == -2
     assert call(eos=100) == -2 and call(eos=-2) == -2 and call(done=FAKE) == -2 and call(rho=float("nan")) == -2
-    for name in ("z", "score", "par", "tok", "so", "ws"):
+    for name in ("z", "score", "par", "tok", "so", "arr", "ws"):
         assert call(**{name: None}) == -1
     assert call(so=FAKE) == -6 and call(done=FAKE, do=FAKE, eos=3) == -6
-    assert call(z=P(4098)) == -3 and call(ws=P(4104)) == -3
+    assert call(z=P(4098)) == -3 and call(ws=P(4104)) == -3 and call(arr=P(4098)) == -3
     need = Bd.workspace_bytes(Bd.WS_LM_SELECT, (2, 4, 100))
     assert need > 0 and call(n=need - 1) == -5
     assert call(B=0) == 0
