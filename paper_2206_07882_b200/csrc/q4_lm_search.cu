@@ -81,7 +81,7 @@ template <> __device__ __forceinline__ uint4 lowest_vector<float>() { return mak
 template <> __device__ __forceinline__ uint4 lowest_vector<__half>() { return make_uint4(0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u); }
 template <> __device__ __forceinline__ uint4 lowest_vector<__nv_bfloat16>() { return make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u); }
 
-constexpr int ROW_NT = 256, ROW_VECTORS = 4, ROW_GROUPS = ROW_NT / 4, ROW_LIST = 512, ROW_STAGES = 3;
+constexpr int ROW_NT = 256, ROW_VECTORS = 4, ROW_GROUPS = ROW_NT / 4, ROW_STAGES = 3, ROW_TURNS = 8, ROW_LIST = 1024;
 constexpr int ROW_TURN = ROW_NT * ROW_VECTORS;                    // 16-byte vectors that a block reads in one turn
 constexpr int ROW_RING = ROW_STAGES * ROW_TURN * 16;              // bytes
 constexpr int MERGE_LIST = 1024;
@@ -119,13 +119,18 @@ __device__ __forceinline__ bool before(const Proposal& a, const Proposal& b) {
 }
 
 struct SelectShared {
-  float value[ROW_LIST];
-  int32_t label[ROW_LIST], vector[ROW_LIST];
+  __nv_bfloat16 turn_top[ROW_TURNS][ROW_NT];   // a thread's maximum of a turn, rounded up
   Best best[64];
   double sum[ROW_NT / 32];
   float group[ROW_GROUPS], top[ROW_NT / 32], scale[ROW_NT / 32];
-  int32_t vectors, n, some, last;
+  int32_t n, last;
 };
+// A segment's candidates lie in the last stage of the ring, which short segments do not reach
+struct CandidateShared {
+  float value[ROW_LIST];
+  int32_t label[ROW_LIST];
+};
+static_assert(sizeof(CandidateShared) <= ROW_TURN * 16, "candidates in one stage");
 // What the merge needs lies where the copies landed (a block's last turn has been waited for by then)
 struct MergeShared {
   double score[MAX_BEAMS], lse[MAX_BEAMS];   // lse NaN: the beam proposes nothing
@@ -161,17 +166,17 @@ __device__ __forceinline__ float group_bound(SelectShared& sh, float mine, int W
   return fminf(sh.top[0], sh.top[1]);
 }
 
-// One pass over a segment: running maximum and sum of every thread, and the candidates for the segment's W best.
-// A bound on those comes from the first turn (group_bound): of the elements behind it only larger ones count (equal ones come
-// later in the order).  About 18 (W = 16) to 45 (W = 32) elements of a turn pass a bound like that.  The loop notes the vectors
-// that hold them; their elements are looked at again and ranked at the end.  A list that overflows (equal or rising logits) is
-// given up for W passes over the segment.
+// One pass over a segment of at most 8 turns: running maximum and sum of every thread, and the thread's maximum of every turn.
+// The W-th best of the maxima of 64 groups of four threads (group_bound) then bounds the segment's W best from below: about 18
+// (W = 16) to 45 (W = 32) elements reach it.  Those turns of a thread that hold one are read again, from the L2, and the candidates
+// ranked.  More candidates than the list takes (equal logits) are given up for W passes over the segment.
 // Every thread copies the vectors it will read itself into shared memory, two turns ahead: no barrier in the loop, no registers
 // for what is on its way, and four blocks of an SM keep 128 KB in flight.
 template <typename T>
 __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const RowParts& p, long long row, int part, SelectShared& sh,
                                                 uint4* ring) {
   constexpr int N = Vec<T>::N;
+  CandidateShared& list = *reinterpret_cast<CandidateShared*>(ring + (ROW_STAGES - 1) * ROW_TURN);
   const int tid = threadIdx.x, W = a.W;
   const T* z = static_cast<const T*>(a.logits) + row * a.ld;
   // elements in front of the first 16-byte boundary, vectors, and elements behind the last whole vector
@@ -179,7 +184,7 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
   const int n_vec = (a.V - head) / N;
   const uint4* body = reinterpret_cast<const uint4*>(z + head);
   const int v0 = min(part * p.vectors, n_vec), v1 = part + 1 == p.parts ? n_vec : min(v0 + p.vectors, n_vec);
-  const int turns = max((v1 - v0 + ROW_TURN - 1) / ROW_TURN, 1);
+  const int turns = (v1 - v0 + ROW_TURN - 1) / ROW_TURN;
   const uint4* src = body + v0 + tid;              // first vector of the next turn to fetch
   int left = v1 - v0 - tid, to_slot = tid;         // vectors from there on; its place in the ring
   auto fetch = [&]() {
@@ -187,7 +192,7 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
     if (left > (ROW_VECTORS - 1) * ROW_NT) {
 #pragma unroll
       for (int j = 0; j < ROW_VECTORS; ++j) copy_async16(slot + j * ROW_NT, src + j * ROW_NT);
-    } else {
+    } else if (left > -tid) {                      // the last turn
 #pragma unroll
       for (int j = 0; j < ROW_VECTORS; ++j)
         if (j * ROW_NT < left)
@@ -207,65 +212,67 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
   if (part == 0 && tid < head) extra_at = tid;
   if (part + 1 == p.parts && tid >= 32 && tid < 32 + a.V - tail) extra_at = tail + tid - 32;
   const float extra = extra_at >= 0 ? to_f32<T>(z[extra_at]) : -INFINITY;
-  if (tid == 0) sh.vectors = sh.n = sh.some = 0;
+  if (tid == 0) sh.n = 0;
 
-  float m = extra != extra ? -INFINITY : extra, scale = sum_scale(m), bound = 0.0f, limit = 0.0f;
+  float m = extra != extra ? -INFINITY : extra, scale = sum_scale(m);
   float sum = exp2_unit(__fmaf_rn(extra, LOG2E, -scale));   // (a NaN makes the sum NaN)
   int from_slot = tid;
   for (int t = 0; t < turns; ++t) {
     copy_async_wait<ROW_STAGES - 2>();
     const uint4* slot = ring + from_slot;
     from_slot = from_slot < (ROW_STAGES - 1) * ROW_TURN ? from_slot + ROW_TURN : tid;
-    float vector_top[ROW_VECTORS], top = -INFINITY;
+    float x[ROW_VECTORS][N], top = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < ROW_VECTORS; ++j) {
-      float x[N];
-      Vec<T>::get(slot[j * ROW_NT], x);
-      vector_top[j] = x[0];
+    for (int j = 0; j < ROW_VECTORS; ++j) Vec<T>::get(slot[j * ROW_NT], x[j]);
 #pragma unroll
-      for (int i = 1; i < N; ++i) vector_top[j] = fmaxf(vector_top[j], x[i]);
-      top = fmaxf(top, vector_top[j]);
-    }
+    for (int j = 0; j < ROW_VECTORS; ++j)
+#pragma unroll
+      for (int i = 0; i < N; ++i) top = fmaxf(top, x[j][i]);
     fetch();
-    if (t == 0) {
-      bound = group_bound(sh, fmaxf(top, m), W);
-      limit = nextafterf(bound, -INFINITY);   // the first turn's elements count from the bound on
-      if (extra > limit) {
-        const int at = atomicAdd(&sh.n, 1);   // (there are at most 14 of these)
-        sh.value[at] = extra;
-        sh.label[at] = extra_at;
-      }
-    }
-    if (top > limit) {
-#pragma unroll
-      for (int j = 0; j < ROW_VECTORS; ++j)
-        if (vector_top[j] > limit) {
-          const int at = atomicAdd(&sh.vectors, 1);
-          if (at < ROW_LIST) sh.vector[at] = v0 + t * ROW_TURN + j * ROW_NT + tid;
-        }
-    }
-    limit = bound;
+    sh.turn_top[t][tid] = __float2bfloat16_ru(top);
     m = fmaxf(m, top);
     const float next = sum_scale(m);
     const uint64_t mul = pk2(LOG2E, LOG2E), sub = pk2(-next, -next);
     uint64_t part_sum = pk2(0.0f, 0.0f);
 #pragma unroll
-    for (int j = 0; j < ROW_VECTORS; ++j) {
-      float x[N];
-      Vec<T>::get(slot[j * ROW_NT], x);
+    for (int j = 0; j < ROW_VECTORS; ++j)
 #pragma unroll
       for (int i = 0; i < N; i += 2) {
         float e0, e1;
-        upk2(fma2(pk2(x[i], x[i + 1]), mul, sub), e0, e1);
+        upk2(fma2(pk2(x[j][i], x[j][i + 1]), mul, sub), e0, e1);
         part_sum = add2(part_sum, pk2(exp2_unit(e0), exp2_unit(e1)));
       }
-    }
     float even, odd;
     upk2(part_sum, even, odd);
     sum = sum * pow2_down(scale - next) + (even + odd);
     scale = next;
   }
 
+  const float bound = group_bound(sh, m, W);
+  // the candidates: elements from the bound on
+  auto offer = [&](float v, int label) {
+    if (v >= bound && v > -INFINITY) {
+      const int at = atomicAdd(&sh.n, 1);
+      if (at < ROW_LIST) {
+        list.value[at] = v;
+        list.label[at] = label;
+      }
+    }
+  };
+  offer(extra, extra_at);
+  for (int t = 0; t < turns; ++t)
+    if (__bfloat162float(sh.turn_top[t][tid]) >= bound) {
+#pragma unroll 1
+      for (int j = 0; j < ROW_VECTORS; ++j) {
+        const int v = t * ROW_TURN + j * ROW_NT + tid;
+        if (v >= v1 - v0) break;
+        float x[N];
+        Vec<T>::get(turns < ROW_STAGES ? ring[v] : __ldg(body + v0 + v), x);
+#pragma unroll
+        for (int i = 0; i < N; ++i) offer(x[i], head + (v0 + v) * N + i);
+      }
+    }
+  // the segment's log-sum-exp
   float top = m, most = scale;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
@@ -283,7 +290,6 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
     top = fmaxf(top, sh.top[w]);
     most = fmaxf(most, sh.scale[w]);
   }
-  const int n_vectors = sh.vectors;
   const bool far = top > -INFINITY && fabsf(top) > 1e6f;
   double total = (double)(sum * pow2_down(scale - most));
   const int from = part == 0 ? 0 : head + v0 * N, to = part + 1 == p.parts ? a.V : head + v1 * N;
@@ -294,25 +300,10 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
   if ((tid & 31) == 0) sh.sum[tid >> 5] = total;
-  // elements of the noted vectors
-  for (int i = tid; i < min(n_vectors, ROW_LIST); i += ROW_NT) {
-    const int v = sh.vector[i];
-    float x[N];
-    Vec<T>::get(turns <= ROW_STAGES ? ring[v - v0] : __ldg(body + v), x);   // (the ring still holds a short segment)
-    limit = v < v0 + ROW_TURN ? nextafterf(bound, -INFINITY) : bound;
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-      if (x[j] > limit) {
-        const int at = atomicAdd(&sh.n, 1);
-        if (at < ROW_LIST) {
-          sh.value[at] = x[j];
-          sh.label[at] = head + v * N + j;
-        }
-      }
-  }
+  const int n = sh.n;
   __syncthreads();
   const long long out = row * p.parts + part;
-  if (tid == ROW_NT - 1) {   // (a warp that has the least to rank)
+  if (tid == ROW_NT - 1) {   // (a warp that has nothing to rank, mostly)
     total = 0.0;
 #pragma unroll
     for (int w = 0; w < ROW_NT / 32; ++w) total += sh.sum[w];
@@ -320,49 +311,20 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
     p.lse[out] = top == -INFINITY ? (total == 0.0 ? -INFINITY : NAN) : base + log(total) - excess;
   }
   Best* best = p.best + out * W;
-  int n = sh.n;
-  if (n_vectors <= ROW_LIST && n <= ROW_LIST) {
-    // those with fewer than W larger ones, W and what is equal to the last of them, into a short list; their places in that
-    if (n + tid < (n + 3) / 4 * 4) sh.value[n + tid] = -INFINITY;
-    __syncthreads();
-    for (int i = tid; i < n; i += ROW_NT) {
-      const float mine = sh.value[i];
-      int larger = 0;
-#pragma unroll 4
-      for (int j = 0; j < n; j += 4) {
-        const float4 o = *reinterpret_cast<const float4*>(sh.value + j);
-        larger += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
+  if (n <= ROW_LIST) {
+    for (int i = tid; i < max(n, W); i += ROW_NT) {
+      if (i >= n) {
+        best[i] = Best{-INFINITY, -1};
+        continue;
       }
-      if (larger < W) {
-        const int at = atomicAdd(&sh.some, 1);
-        if (at < 64) sh.best[at] = Best{mine, sh.label[i]};
-      }
-    }
-    __syncthreads();
-    n = sh.some;
-    if (n <= 64) {
-      if (tid < max(n, W)) {
-        if (tid >= n) {
-          best[tid] = Best{-INFINITY, -1};
-        } else {
-          const Best mine = sh.best[tid];
-          int rank = 0;
-#pragma unroll 4
-          for (int j = 0; j < n; ++j) rank += before(sh.best[j].value, sh.best[j].label, mine.value, mine.label);
-          if (rank < W) best[rank] = mine;
-        }
-      }
-      return;
-    }
-    n = sh.n;
-    for (int i = tid; i < n; i += ROW_NT) {   // many equal ones
-      const float mine = sh.value[i];
-      const int label = sh.label[i];
+      const float mine = list.value[i];
+      const int label = list.label[i];
       int rank = 0;
-      for (int j = 0; j < n; ++j) rank += before(sh.value[j], sh.label[j], mine, label);
+#pragma unroll 8
+      for (int j = 0; j < n; ++j) rank += before(list.value[j], list.label[j], mine, label);
       if (rank < W) best[rank] = Best{mine, label};
     }
-    return;                                    // (more than 64 elements, so W of them)
+    return;
   }
   Best last{INFINITY, -1};
   for (int i = 0; i < W; ++i) {
@@ -591,7 +553,7 @@ static RowParts row_parts(int B, int W, int V, int bytes, uint8_t* workspace) {
   const int per_block = ROW_TURN * (16 / bytes);                  // elements of one turn of a block
   const long long fill = (4LL * sm_count() + rows - 1) / rows;
   long long parts = ((long long)V + per_block - 1) / per_block;
-  const long long least = (parts + 7) / 8;
+  const long long least = (parts + ROW_TURNS - 1) / ROW_TURNS;
   parts = parts < fill ? parts : fill;
   parts = parts > least ? parts : least;
   RowParts p;
