@@ -81,16 +81,10 @@ template <> __device__ __forceinline__ uint4 lowest_vector<float>() { return mak
 template <> __device__ __forceinline__ uint4 lowest_vector<__half>() { return make_uint4(0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u); }
 template <> __device__ __forceinline__ uint4 lowest_vector<__nv_bfloat16>() { return make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u); }
 
-constexpr int ROW_NT = 256, ROW_VECTORS = 4, ROW_GROUPS = ROW_NT / 4, ROW_STAGES = 3, ROW_TURNS = 8, ROW_LIST = 1024;
-constexpr int ROW_TURN = ROW_NT * ROW_VECTORS;                    // 16-byte vectors that a block reads in one turn
-constexpr int ROW_RING = ROW_STAGES * ROW_TURN * 16;              // bytes
-constexpr int MERGE_LIST = 1024;
-
-__device__ __forceinline__ void copy_async16(uint4* dst, const uint4* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
-}
-__device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int LEFT> __device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+constexpr int ROW_NT = 128, ROW_BLOCKS = 8;       // threads of a block, blocks of an SM
+constexpr int ROW_VECTORS = 4, ROW_TURNS = 16, ROW_GROUPS = 64;
+constexpr int ROW_TURN = ROW_NT * ROW_VECTORS;    // 16-byte vectors that a block reads in one turn
+constexpr int ROW_NOTED = 512, ROW_LIST = 1024, MERGE_LIST = 512;
 
 // Sums of exponentials are kept as s 2^n, n an integer: a term is 2^(x log2 e - n), one fused multiply-add and the base-2 unit,
 // and a change of n is exact.  The rounded constant raises e to 1 + LOG2E_EXCESS, which is taken out again at the maximum.
@@ -118,20 +112,12 @@ __device__ __forceinline__ bool before(const Proposal& a, const Proposal& b) {
   return a.key > b.key || (a.key == b.key && (a.beam < b.beam || (a.beam == b.beam && before(a.z, a.label, b.z, b.label))));
 }
 
-struct SelectShared {
-  __nv_bfloat16 turn_top[ROW_TURNS][ROW_NT];   // a thread's maximum of a turn, rounded up
-  Best best[64];
-  double sum[ROW_NT / 32];
-  float group[ROW_GROUPS], top[ROW_NT / 32], scale[ROW_NT / 32];
-  int32_t n, last;
-};
-// A segment's candidates lie in the last stage of the ring, which short segments do not reach
-struct CandidateShared {
-  float value[ROW_LIST];
+struct RowShared {            // of a segment
+  uint4 vector[ROW_NOTED];    // noted vectors of logits, and their numbers
+  int32_t number[ROW_NOTED];
+  float value[ROW_LIST];      // candidates
   int32_t label[ROW_LIST];
 };
-static_assert(sizeof(CandidateShared) <= ROW_TURN * 16, "candidates in one stage");
-// What the merge needs lies where the copies landed (a block's last turn has been waited for by then)
 struct MergeShared {
   double score[MAX_BEAMS], lse[MAX_BEAMS];   // lse NaN: the beam proposes nothing
   int32_t ended[MAX_BEAMS];
@@ -139,15 +125,27 @@ struct MergeShared {
   float z[MERGE_LIST];
   int32_t label[MERGE_LIST], beam[MERGE_LIST];
 };
-static_assert(sizeof(MergeShared) <= (size_t)ROW_RING && MERGE_LIST >= ROW_NT, "the merge's shared memory");
+struct SelectShared {
+  union {
+    RowShared row;
+    MergeShared merge;
+  };
+  Best best[ROW_NT / 32];
+  double sum[ROW_NT / 32];
+  float group[ROW_GROUPS], top[ROW_NT / 32], scale[ROW_NT / 32], bound[2];
+  int32_t noted, n, last;
+};
+static_assert(MERGE_LIST >= ROW_NT && sizeof(SelectShared) * ROW_BLOCKS <= 200 * 1024, "shared memory of an SM");
 
 // The W-th largest of the block's ROW_GROUPS group maxima, at least (W of the elements are no smaller): every thread of the first
 // two warps counts what is larger than its own, and the smallest of those with fewer than W larger ones is taken.
 __device__ __forceinline__ float group_bound(SelectShared& sh, float mine, int W) {
-  mine = fmaxf(mine, __shfl_xor_sync(0xffffffffu, mine, 1));
-  mine = fmaxf(mine, __shfl_xor_sync(0xffffffffu, mine, 2));
+  constexpr int EACH = ROW_NT / ROW_GROUPS;
+  static_assert(ROW_GROUPS == 64 && EACH >= 1 && EACH <= 32, "two warps count, groups lie within a warp");
+#pragma unroll
+  for (int o = 1; o < EACH; o <<= 1) mine = fmaxf(mine, __shfl_xor_sync(0xffffffffu, mine, o));
   const int tid = threadIdx.x;
-  if ((tid & 3) == 0) sh.group[tid >> 2] = mine;
+  if (tid % EACH == 0) sh.group[tid / EACH] = mine;
   __syncthreads();
   if (tid < ROW_GROUPS) {
     mine = sh.group[tid];
@@ -160,96 +158,111 @@ __device__ __forceinline__ float group_bound(SelectShared& sh, float mine, int W
     float low = larger < W ? mine : INFINITY;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) low = fminf(low, __shfl_xor_sync(0xffffffffu, low, o));
-    if ((tid & 31) == 0) sh.top[tid >> 5] = low;
+    if ((tid & 31) == 0) sh.bound[tid >> 5] = low;
   }
   __syncthreads();
-  return fminf(sh.top[0], sh.top[1]);
+  return fminf(sh.bound[0], sh.bound[1]);
 }
 
-// One pass over a segment of at most 8 turns: running maximum and sum of every thread, and the thread's maximum of every turn.
-// The W-th best of the maxima of 64 groups of four threads (group_bound) then bounds the segment's W best from below: about 18
-// (W = 16) to 45 (W = 32) elements reach it.  Those turns of a thread that hold one are read again, from the L2, and the candidates
-// ranked.  More candidates than the list takes (equal logits) are given up for W passes over the segment.
-// Every thread copies the vectors it will read itself into shared memory, two turns ahead: no barrier in the loop, no registers
-// for what is on its way, and four blocks of an SM keep 128 KB in flight.
+// One pass over a segment of at most 16 turns: running maximum and sum of every thread, and the segment's candidates.
+// The W-th best of the running maxima of 64 groups of threads (group_bound), taken after turns 1, 2, 4, 8 and 16, bounds the
+// segment's W best from below.  Vectors with an element above it are noted: of the turn that it was taken in also those that
+// reach it, W of which are no smaller; behind that turn only larger ones, as equal ones come later in the order.  About 18 (W = 16) to 45
+// (W = 32) elements pass between two bounds.  The noted vectors' elements that reach the last bound are ranked.  More than the
+// lists take (equal or rising logits) are given up for W passes over the segment.
+// The next turn's vectors are on their way into registers while a turn is worked on: 64 KB in eight blocks of an SM.
+// (Candidates read again once the last bound was known took 14 of 60 us at 64 x 16 x 32768 fp32, a bound of the first turn
+// alone 9 of 44; two turns ahead in shared memory by asynchronous copies was no faster than one in registers.)
 template <typename T>
-__device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const RowParts& p, long long row, int part, SelectShared& sh,
-                                                uint4* ring) {
+__device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const RowParts& p, long long row, int part, SelectShared& sh) {
   constexpr int N = Vec<T>::N;
-  CandidateShared& list = *reinterpret_cast<CandidateShared*>(ring + (ROW_STAGES - 1) * ROW_TURN);
+  RowShared& list = sh.row;
   const int tid = threadIdx.x, W = a.W;
   const T* z = static_cast<const T*>(a.logits) + row * a.ld;
   // elements in front of the first 16-byte boundary, vectors, and elements behind the last whole vector
   const int head = min((int)(((16 - (reinterpret_cast<uintptr_t>(z) & 15)) & 15) / sizeof(T)), a.V);
   const int n_vec = (a.V - head) / N;
-  const uint4* body = reinterpret_cast<const uint4*>(z + head);
   const int v0 = min(part * p.vectors, n_vec), v1 = part + 1 == p.parts ? n_vec : min(v0 + p.vectors, n_vec);
   const int turns = (v1 - v0 + ROW_TURN - 1) / ROW_TURN;
-  const uint4* src = body + v0 + tid;              // first vector of the next turn to fetch
-  int left = v1 - v0 - tid, to_slot = tid;         // vectors from there on; its place in the ring
+  const uint4* src = reinterpret_cast<const uint4*>(z + head) + v0 + tid;
+  int left = v1 - v0 - tid;                        // vectors from src on
+  uint4 next[ROW_VECTORS];
   auto fetch = [&]() {
-    uint4* slot = ring + to_slot;
     if (left > (ROW_VECTORS - 1) * ROW_NT) {
 #pragma unroll
-      for (int j = 0; j < ROW_VECTORS; ++j) copy_async16(slot + j * ROW_NT, src + j * ROW_NT);
-    } else if (left > -tid) {                      // the last turn
+      for (int j = 0; j < ROW_VECTORS; ++j) next[j] = __ldg(src + j * ROW_NT);
+    } else {
 #pragma unroll
-      for (int j = 0; j < ROW_VECTORS; ++j)
-        if (j * ROW_NT < left)
-          copy_async16(slot + j * ROW_NT, src + j * ROW_NT);
-        else
-          slot[j * ROW_NT] = lowest_vector<T>();
+      for (int j = 0; j < ROW_VECTORS; ++j) next[j] = j * ROW_NT < left ? __ldg(src + j * ROW_NT) : lowest_vector<T>();
     }
-    copy_async_commit();
     src += ROW_TURN;
     left -= ROW_TURN;
-    to_slot = to_slot < (ROW_STAGES - 1) * ROW_TURN ? to_slot + ROW_TURN : tid;
   };
-#pragma unroll
-  for (int t = 0; t < ROW_STAGES - 1; ++t) fetch();
+  fetch();
   const int tail = head + n_vec * N;
-  int extra_at = -1;
-  if (part == 0 && tid < head) extra_at = tid;
-  if (part + 1 == p.parts && tid >= 32 && tid < 32 + a.V - tail) extra_at = tail + tid - 32;
-  const float extra = extra_at >= 0 ? to_f32<T>(z[extra_at]) : -INFINITY;
-  if (tid == 0) sh.n = 0;
+  const float first = part == 0 && tid < head ? to_f32<T>(z[tid]) : -INFINITY;
+  const float last = part + 1 == p.parts && tid < a.V - tail ? to_f32<T>(z[tail + tid]) : -INFINITY;
+  if (tid == 0) sh.n = sh.noted = 0;
 
-  float m = extra != extra ? -INFINITY : extra, scale = sum_scale(m);
-  float sum = exp2_unit(__fmaf_rn(extra, LOG2E, -scale));   // (a NaN makes the sum NaN)
-  int from_slot = tid;
+  float m = first != first ? -INFINITY : first, scale = sum_scale(m), bound = -INFINITY, limit = -INFINITY;
+  float sum = exp2_unit(__fmaf_rn(first, LOG2E, -scale));   // (a NaN makes the sum NaN)
   for (int t = 0; t < turns; ++t) {
-    copy_async_wait<ROW_STAGES - 2>();
-    const uint4* slot = ring + from_slot;
-    from_slot = from_slot < (ROW_STAGES - 1) * ROW_TURN ? from_slot + ROW_TURN : tid;
-    float x[ROW_VECTORS][N], top = -INFINITY;
+    uint4 raw[ROW_VECTORS];
+    float vector_top[ROW_VECTORS], top = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < ROW_VECTORS; ++j) Vec<T>::get(slot[j * ROW_NT], x[j]);
-#pragma unroll
-    for (int j = 0; j < ROW_VECTORS; ++j)
-#pragma unroll
-      for (int i = 0; i < N; ++i) top = fmaxf(top, x[j][i]);
+    for (int j = 0; j < ROW_VECTORS; ++j) raw[j] = next[j];
     fetch();
-    sh.turn_top[t][tid] = __float2bfloat16_ru(top);
+#pragma unroll
+    for (int j = 0; j < ROW_VECTORS; ++j) {
+      float x[N];
+      Vec<T>::get(raw[j], x);
+      vector_top[j] = x[0];
+#pragma unroll
+      for (int i = 1; i < N; ++i) vector_top[j] = fmaxf(vector_top[j], x[i]);
+      top = fmaxf(top, vector_top[j]);
+    }
     m = fmaxf(m, top);
-    const float next = sum_scale(m);
-    const uint64_t mul = pk2(LOG2E, LOG2E), sub = pk2(-next, -next);
+    if ((t & (t + 1)) == 0) {
+      bound = group_bound(sh, m, W);
+      limit = nextafterf(bound, -INFINITY);
+    }
+    if (top > limit) {
+#pragma unroll
+      for (int j = 0; j < ROW_VECTORS; ++j)
+        if (vector_top[j] > limit) {
+          const int at = atomicAdd(&sh.noted, 1);
+          if (at < ROW_NOTED) {
+            list.vector[at] = raw[j];
+            list.number[at] = v0 + t * ROW_TURN + j * ROW_NT + tid;
+          }
+        }
+    }
+    limit = bound;
+    const float now = sum_scale(m);
+    const uint64_t mul = pk2(LOG2E, LOG2E), sub = pk2(-now, -now);
     uint64_t part_sum = pk2(0.0f, 0.0f);
 #pragma unroll
-    for (int j = 0; j < ROW_VECTORS; ++j)
+    for (int j = 0; j < ROW_VECTORS; ++j) {
+      float x[N];
+      Vec<T>::get(raw[j], x);
 #pragma unroll
       for (int i = 0; i < N; i += 2) {
         float e0, e1;
-        upk2(fma2(pk2(x[j][i], x[j][i + 1]), mul, sub), e0, e1);
+        upk2(fma2(pk2(x[i], x[i + 1]), mul, sub), e0, e1);
         part_sum = add2(part_sum, pk2(exp2_unit(e0), exp2_unit(e1)));
       }
+    }
     float even, odd;
     upk2(part_sum, even, odd);
-    sum = sum * pow2_down(scale - next) + (even + odd);
-    scale = next;
+    sum = sum * pow2_down(scale - now) + (even + odd);
+    scale = now;
   }
+  m = fmaxf(m, last);
+  const float now = sum_scale(m);
+  sum = sum * pow2_down(scale - now) + exp2_unit(__fmaf_rn(last, LOG2E, -now));
+  scale = now;
 
-  const float bound = group_bound(sh, m, W);
-  // the candidates: elements from the bound on
+  // candidates: elements that reach the last bound (without turns there is none)
   auto offer = [&](float v, int label) {
     if (v >= bound && v > -INFINITY) {
       const int at = atomicAdd(&sh.n, 1);
@@ -259,19 +272,17 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
       }
     }
   };
-  offer(extra, extra_at);
-  for (int t = 0; t < turns; ++t)
-    if (__bfloat162float(sh.turn_top[t][tid]) >= bound) {
-#pragma unroll 1
-      for (int j = 0; j < ROW_VECTORS; ++j) {
-        const int v = t * ROW_TURN + j * ROW_NT + tid;
-        if (v >= v1 - v0) break;
-        float x[N];
-        Vec<T>::get(turns < ROW_STAGES ? ring[v] : __ldg(body + v0 + v), x);
+  __syncthreads();
+  const int noted = sh.noted;
+  offer(first, tid);
+  offer(last, tail + tid);
+  for (int i = tid; i < min(noted, ROW_NOTED); i += ROW_NT) {
+    float x[N];
+    Vec<T>::get(list.vector[i], x);
+    const int label = head + list.number[i] * N;
 #pragma unroll
-        for (int i = 0; i < N; ++i) offer(x[i], head + (v0 + v) * N + i);
-      }
-    }
+    for (int j = 0; j < N; ++j) offer(x[j], label + j);
+  }
   // the segment's log-sum-exp
   float top = m, most = scale;
 #pragma unroll
@@ -279,7 +290,6 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
   }
-  __syncthreads();                             // (the bound has been read)
   if ((tid & 31) == 0) {
     sh.top[tid >> 5] = top;
     sh.scale[tid >> 5] = most;
@@ -311,7 +321,7 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
     p.lse[out] = top == -INFINITY ? (total == 0.0 ? -INFINITY : NAN) : base + log(total) - excess;
   }
   Best* best = p.best + out * W;
-  if (n <= ROW_LIST) {
+  if (noted <= ROW_NOTED && n <= ROW_LIST) {
     for (int i = tid; i < max(n, W); i += ROW_NT) {
       if (i >= n) {
         best[i] = Best{-INFINITY, -1};
@@ -326,12 +336,12 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
     }
     return;
   }
-  Best last{INFINITY, -1};
+  Best before_it{INFINITY, -1};
   for (int i = 0; i < W; ++i) {
     Best b{-INFINITY, INT32_MAX};
     for (int k = from + tid; k < to; k += ROW_NT) {
       const float f = to_f32<T>(z[k]);
-      if (f > -INFINITY && before(last.value, last.label, f, k) && before(f, k, b.value, b.label)) b = Best{f, k};
+      if (f > -INFINITY && before(before_it.value, before_it.label, f, k) && before(f, k, b.value, b.label)) b = Best{f, k};
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
@@ -344,7 +354,7 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
     for (int w = 0; w < ROW_NT / 32; ++w)
       if (before(sh.best[w].value, sh.best[w].label, b.value, b.label)) b = sh.best[w];
     if (tid == 0) best[i] = b.label == INT32_MAX ? Best{-INFINITY, -1} : b;   // (overflowed: there are more than W)
-    last = b;
+    before_it = b;
   }
 }
 
@@ -352,7 +362,8 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
 // segments' shares of lse are put together first.  As for a segment a bound from group maxima (rounded down to fp32, so it errs
 // on the safe side) leaves few proposals to rank.  Every entry of the lists has a thread of its own where there are enough: a walk
 // down the lists took 20 us in dependent loads.
-__device__ __forceinline__ void merge_segments(const LmSelectArgs& a, const RowParts& p, int utterance, SelectShared& sh, MergeShared& mg) {
+__device__ __forceinline__ void merge_segments(const LmSelectArgs& a, const RowParts& p, int utterance, SelectShared& sh) {
+  MergeShared& mg = sh.merge;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, W = a.W;
   const long long row0 = (long long)utterance * W;
   // entry ((w parts + i) W + j): place j of segment i of beam w
@@ -479,14 +490,13 @@ __device__ __forceinline__ void merge_segments(const LmSelectArgs& a, const RowP
 // what its threads wrote (a barrier and a fence before the count), the last one reads the others' after the count and a fence, past
 // the L1.  The count wraps to 0 for the next call.
 template <typename T>
-__global__ void __launch_bounds__(ROW_NT, 4) k_lm_select(const LmSelectArgs a, const RowParts p) {
-  extern __shared__ uint4 s_ring[];
+__global__ void __launch_bounds__(ROW_NT, ROW_BLOCKS) k_lm_select(const LmSelectArgs a, const RowParts p) {
   __shared__ __align__(16) SelectShared sh;
   const long long row = blockIdx.x / p.parts;
   const int part = blockIdx.x % p.parts, utterance = (int)(row / a.W);
   pdl_wait();
   pdl_trigger();   // (nothing of a later kernel starts to read or write before this grid has ended)
-  if (isfinite(a.score[row]) && !(a.done && a.done[row])) best_of_segment<T>(a, p, row, part, sh, s_ring);
+  if (isfinite(a.score[row]) && !(a.done && a.done[row])) best_of_segment<T>(a, p, row, part, sh);
   __syncthreads();
   if (threadIdx.x == 0) {
     const uint32_t blocks = (uint32_t)a.W * p.parts;
@@ -495,7 +505,7 @@ __global__ void __launch_bounds__(ROW_NT, 4) k_lm_select(const LmSelectArgs a, c
     __threadfence();
   }
   __syncthreads();
-  if (sh.last) merge_segments(a, p, utterance, sh, *reinterpret_cast<MergeShared*>(s_ring));
+  if (sh.last) merge_segments(a, p, utterance, sh);
 }
 
 // Moves of up to Q4_REORDER_MAX tensors, cut into vectors of `width` bytes.
@@ -546,16 +556,12 @@ __global__ void __launch_bounds__(256) k_beam_reorder(const __grid_constant__ Mo
 
 }  // namespace
 
-// Segments of a row: at least as many as keep their lists short (8 bounds of 4096 elements, see k_lm_select), and more while there
-// are fewer than 4 blocks per SM and segments of more than one such bound; they are as long as one another.
 static RowParts row_parts(int B, int W, int V, int bytes, uint8_t* workspace) {
-  const long long rows = (long long)B * W;
-  const int per_block = ROW_TURN * (16 / bytes);                  // elements of one turn of a block
-  const long long fill = (4LL * sm_count() + rows - 1) / rows;
-  long long parts = ((long long)V + per_block - 1) / per_block;
-  const long long least = (parts + ROW_TURNS - 1) / ROW_TURNS;
-  parts = parts < fill ? parts : fill;
-  parts = parts > least ? parts : least;
+  const long long rows = (long long)B * W, slots = (long long)ROW_BLOCKS * sm_count();
+  const long long turns = ((long long)V + ROW_TURN * (16 / bytes) - 1) / (ROW_TURN * (16 / bytes)), least = (turns + ROW_TURNS - 1) / ROW_TURNS;
+  long long parts = slots / rows;
+  if (parts > turns) parts = turns;
+  if (parts < least) parts = least;
   RowParts p;
   p.parts = (int)parts;
   const long long vectors = (V * (long long)bytes + 15) / 16;
@@ -577,14 +583,7 @@ size_t lm_select_workspace(int B, int W, int V) {
 
 template <typename T>
 static cudaError_t launch_select(const LmSelectArgs& a, const RowParts& p, cudaStream_t s) {
-  static bool configured_on[MAX_DEVICES];
-  bool& configured = configured_on[device_slot()];
-  if (!configured) {
-    const cudaError_t e = cudaFuncSetAttribute(k_lm_select<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, ROW_RING);
-    if (e != cudaSuccess) return e;
-    configured = true;
-  }
-  return launch_ex(k_lm_select<T>, dim3((unsigned)((long long)a.B * a.W * p.parts)), dim3(ROW_NT), ROW_RING, s, true, 1, a, p);
+  return launch_ex(k_lm_select<T>, dim3((unsigned)((long long)a.B * a.W * p.parts)), dim3(ROW_NT), 0, s, true, 1, a, p);
 }
 cudaError_t launch_lm_select(const LmSelectArgs& a, int dtype, cudaStream_t s) {
   const RowParts p = row_parts(a.B, a.W, a.V, dtype == Q4_F32 ? 4 : 2, a.workspace);
