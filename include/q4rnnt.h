@@ -464,7 +464,7 @@ int q4_linear_token_scales(const void* xq, const float* x_scale, int32_t M, cons
  * A logit of -inf is a label that is not proposed.  A row that holds a NaN or +inf, or nothing but -inf, proposes nothing.
  * Sums, scores and comparisons are carried out in double (exponentials in fp32), whatever dtype is; proposals whose score
  * lies below the range of fp32 are none.  W <= 32, V < 2^31.  No output may be an input.
- *   arrived [B]: counters, zero before the first call; every call leaves them zero.  workspace: q4_workspace_bytes(
+ *   arrived [B (W + 1)]: counters, zero before the first call; every call leaves them zero.  workspace: q4_workspace_bytes(
  *   Q4_WS_LM_SELECT, {B, W, V}) bytes, any contents.  Calls that may overlap need counters and a workspace each.
  */
 int q4_lm_beam_select(const void* logits, int64_t logits_stride, int32_t dtype, const float* score, const uint8_t* done,

@@ -612,11 +612,11 @@ def q4_linear_token_scales(xq: torch.Tensor, x_scale: torch.Tensor, lin: DeviceL
 _select_scratch: dict = {}
 
 
-def _scratch_of_select(like: torch.Tensor, dev: int, stream: int, B: int, need: int) -> tuple:
+def _scratch_of_select(like: torch.Tensor, dev: int, stream: int, counters: int, need: int) -> tuple:
     entry = _select_scratch.get((dev, stream))
     capturing = _capturing()
-    if capturing or entry is None or entry[0].shape[0] < B or entry[1].shape[0] < need:
-        new = like.new_zeros((max(B, 64),), dtype=torch.int32), like.new_empty((need,), dtype=torch.uint8)
+    if capturing or entry is None or entry[0].shape[0] < counters or entry[1].shape[0] < need:
+        new = like.new_zeros((max(counters, 1024),), dtype=torch.int32), like.new_empty((need,), dtype=torch.uint8)
         if capturing:
             return new
         if entry is None and len(_select_scratch) >= _SCRATCH_STREAMS:
@@ -645,7 +645,7 @@ def q4_lm_beam_select(logits: torch.Tensor, score: torch.Tensor, done: Optional[
     if (s[2] != 1 and V > 1) or (B * W > 1 and ld < V) or (B > 1 and s[0] != W * ld):
         raise ValueError("logits: contiguous rows at one distance, beams within utterances")
     stream = torch._C._cuda_getCurrentRawStream(dev)
-    arrived, scratch = _scratch_of_select(score, dev, stream, B, workspace_bytes(WS_LM_SELECT, (B, W, V)))
+    arrived, scratch = _scratch_of_select(score, dev, stream, B * (W + 1), workspace_bytes(WS_LM_SELECT, (B, W, V)))
     if workspace is None:
         workspace = scratch
     ints = score.new_empty((2, B, W), dtype=torch.int32).unbind(0)

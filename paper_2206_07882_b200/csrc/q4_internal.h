@@ -350,7 +350,7 @@ struct LmSelectArgs {
   float* score_out;
   uint8_t* done_out;        // nullable
   uint8_t* workspace;
-  uint32_t* arrived;        // [B] blocks of an utterance that are through; 0 between calls
+  uint32_t* arrived;        // [B] rows of an utterance, [B W] blocks of a row that are through; 0 between calls
 };
 size_t lm_select_workspace(int B, int W, int V);
 cudaError_t launch_lm_select(const LmSelectArgs& a, int dtype, cudaStream_t s);

@@ -12,6 +12,12 @@ namespace {
 
 constexpr int MAX_BEAMS = 32;
 
+// (a NaN loses against a number)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 // 2^x on the base-2 unit (ex2.approx: relative error 2^-22), results below 2^-126 are 0: terms of a sum that has a term of 1
 __device__ __forceinline__ float exp2_unit(float x) {
   float y;
@@ -84,7 +90,7 @@ template <> __device__ __forceinline__ uint4 lowest_vector<__nv_bfloat16>() { re
 constexpr int ROW_NT = 128, ROW_BLOCKS = 8;       // threads of a block, blocks of an SM
 constexpr int ROW_VECTORS = 4, ROW_TURNS = 16, ROW_GROUPS = 64;
 constexpr int ROW_TURN = ROW_NT * ROW_VECTORS;    // 16-byte vectors that a block reads in one turn
-constexpr int ROW_NOTED = 512, ROW_LIST = 1024, MERGE_LIST = 512;
+constexpr int ROW_NOTED = 512, ROW_LIST = 1024, MERGE_LIST = MAX_BEAMS * MAX_BEAMS;
 
 // Sums of exponentials are kept as s 2^n, n an integer: a term is 2^(x log2 e - n), one fused multiply-add and the base-2 unit,
 // and a change of n is exact.  The rounded constant raises e to 1 + LOG2E_EXCESS, which is taken out again at the maximum.
@@ -135,7 +141,7 @@ struct SelectShared {
   float group[ROW_GROUPS], top[ROW_NT / 32], scale[ROW_NT / 32], bound[2];
   int32_t noted, n, last;
 };
-static_assert(MERGE_LIST >= ROW_NT && sizeof(SelectShared) * ROW_BLOCKS <= 200 * 1024, "shared memory of an SM");
+static_assert(sizeof(SelectShared) * ROW_BLOCKS <= 200 * 1024, "shared memory of an SM");
 
 // The W-th largest of the block's ROW_GROUPS group maxima, at least (W of the elements are no smaller): every thread of the first
 // two warps counts what is larger than its own, and the smallest of those with fewer than W larger ones is taken.
@@ -164,13 +170,66 @@ __device__ __forceinline__ float group_bound(SelectShared& sh, float mine, int W
   return fminf(sh.bound[0], sh.bound[1]);
 }
 
-// One pass over a segment of at most 16 turns: running maximum and sum of every thread, and the segment's candidates.
-// The W-th best of the running maxima of 64 groups of threads (group_bound), taken after turns 1, 2, 4, 8 and 16, bounds the
+// The candidates of sh.row that reach `bound`, all of them offered before, as the list `best` of the W best; false if there are more
+// than the list holds.
+__device__ __forceinline__ void offer_candidate(SelectShared& sh, float bound, float v, int label) {
+  if (v >= bound && v > -INFINITY) {
+    const int at = atomicAdd(&sh.n, 1);
+    if (at < ROW_LIST) {
+      sh.row.value[at] = v;
+      sh.row.label[at] = label;
+    }
+  }
+}
+__device__ __forceinline__ bool rank_candidates(const SelectShared& sh, int n, int W, Best* best) {
+  if (n > ROW_LIST) return false;
+  for (int i = threadIdx.x; i < max(n, W); i += ROW_NT) {
+    if (i >= n) {
+      best[i] = Best{-INFINITY, -1};
+      continue;
+    }
+    const float mine = sh.row.value[i];
+    const int label = sh.row.label[i];
+    int rank = 0;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) rank += before(sh.row.value[j], sh.row.label[j], mine, label);
+    if (rank < W) best[rank] = Best{mine, label};
+  }
+  return true;
+}
+// The same by W passes over get(from) .. get(to - 1)
+template <typename F>
+__device__ __forceinline__ void best_by_passes(SelectShared& sh, F get, int from, int to, int W, Best* best) {
+  const int tid = threadIdx.x;
+  Best last{INFINITY, -1};
+  for (int i = 0; i < W; ++i) {
+    Best b{-INFINITY, INT32_MAX};
+    for (int k = from + tid; k < to; k += ROW_NT) {
+      const Best c = get(k);
+      if (c.value > -INFINITY && before(last.value, last.label, c.value, c.label) && before(c.value, c.label, b.value, b.label)) b = c;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const Best c{__shfl_xor_sync(0xffffffffu, b.value, o), __shfl_xor_sync(0xffffffffu, b.label, o)};
+      if (before(c.value, c.label, b.value, b.label)) b = c;
+    }
+    __syncthreads();
+    if ((tid & 31) == 0) sh.best[tid >> 5] = b;
+    __syncthreads();
+    for (int w = 0; w < ROW_NT / 32; ++w)
+      if (before(sh.best[w].value, sh.best[w].label, b.value, b.label)) b = sh.best[w];
+    if (tid == 0) best[i] = b.label == INT32_MAX ? Best{-INFINITY, -1} : b;
+    last = b;
+  }
+}
+
+// One pass over a segment of at most 8 turns: running maximum and sum of every thread, and the segment's candidates.
+// The W-th best of the running maxima of 64 groups of threads (group_bound), taken in turns 1, 2, 4 and 8, bounds the
 // segment's W best from below.  Vectors with an element above it are noted: of the turn that it was taken in also those that
 // reach it, W of which are no smaller; behind that turn only larger ones, as equal ones come later in the order.  About 18 (W = 16) to 45
 // (W = 32) elements pass between two bounds.  The noted vectors' elements that reach the last bound are ranked.  More than the
 // lists take (equal or rising logits) are given up for W passes over the segment.
-// The next turn's vectors are on their way into registers while a turn is worked on: 64 KB in eight blocks of an SM.
+// The next turn's vectors are on their way into registers while a turn is worked on: 80 KB in the five blocks of an SM.
 // (Candidates read again once the last bound was known took 14 of 60 us at 64 x 16 x 32768 fp32, a bound of the first turn
 // alone 9 of 44; two turns ahead in shared memory by asynchronous copies was no faster than one in registers.)
 template <typename T>
@@ -186,19 +245,19 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
   const int turns = (v1 - v0 + ROW_TURN - 1) / ROW_TURN;
   const uint4* src = reinterpret_cast<const uint4*>(z + head) + v0 + tid;
   int left = v1 - v0 - tid;                        // vectors from src on
-  uint4 next[ROW_VECTORS];
-  auto fetch = [&]() {
+  auto fetch = [&](uint4 (&raw)[ROW_VECTORS]) {
     if (left > (ROW_VECTORS - 1) * ROW_NT) {
 #pragma unroll
-      for (int j = 0; j < ROW_VECTORS; ++j) next[j] = __ldg(src + j * ROW_NT);
+      for (int j = 0; j < ROW_VECTORS; ++j) raw[j] = __ldg(src + j * ROW_NT);
     } else {
 #pragma unroll
-      for (int j = 0; j < ROW_VECTORS; ++j) next[j] = j * ROW_NT < left ? __ldg(src + j * ROW_NT) : lowest_vector<T>();
+      for (int j = 0; j < ROW_VECTORS; ++j) raw[j] = j * ROW_NT < left ? __ldg(src + j * ROW_NT) : lowest_vector<T>();
     }
     src += ROW_TURN;
     left -= ROW_TURN;
   };
-  fetch();
+  uint4 raw_a[ROW_VECTORS], raw_b[ROW_VECTORS];
+  fetch(raw_a);
   const int tail = head + n_vec * N;
   const float first = part == 0 && tid < head ? to_f32<T>(z[tid]) : -INFINITY;
   const float last = part + 1 == p.parts && tid < a.V - tail ? to_f32<T>(z[tail + tid]) : -INFINITY;
@@ -206,21 +265,19 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
 
   float m = first != first ? -INFINITY : first, scale = sum_scale(m), bound = -INFINITY, limit = -INFINITY;
   float sum = exp2_unit(__fmaf_rn(first, LOG2E, -scale));   // (a NaN makes the sum NaN)
-  for (int t = 0; t < turns; ++t) {
-    uint4 raw[ROW_VECTORS];
+  auto turn = [&](const uint4 (&raw)[ROW_VECTORS], int t) {
     float vector_top[ROW_VECTORS], top = -INFINITY;
-#pragma unroll
-    for (int j = 0; j < ROW_VECTORS; ++j) raw[j] = next[j];
-    fetch();
 #pragma unroll
     for (int j = 0; j < ROW_VECTORS; ++j) {
       float x[N];
       Vec<T>::get(raw[j], x);
-      vector_top[j] = x[0];
+      vector_top[j] = max3(x[0], x[1], x[2]);
 #pragma unroll
-      for (int i = 1; i < N; ++i) vector_top[j] = fmaxf(vector_top[j], x[i]);
-      top = fmaxf(top, vector_top[j]);
+      for (int i = 3; i + 1 < N; i += 2) vector_top[j] = max3(vector_top[j], x[i], x[i + 1]);
+      vector_top[j] = fmaxf(vector_top[j], x[N - 1]);
     }
+#pragma unroll
+    for (int j = 0; j < ROW_VECTORS; j += 2) top = max3(top, vector_top[j], vector_top[j + 1]);
     m = fmaxf(m, top);
     if ((t & (t + 1)) == 0) {
       bound = group_bound(sh, m, W);
@@ -240,7 +297,7 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
     limit = bound;
     const float now = sum_scale(m);
     const uint64_t mul = pk2(LOG2E, LOG2E), sub = pk2(-now, -now);
-    uint64_t part_sum = pk2(0.0f, 0.0f);
+    uint64_t part_sum[2] = {pk2(0.0f, 0.0f), pk2(0.0f, 0.0f)};
 #pragma unroll
     for (int j = 0; j < ROW_VECTORS; ++j) {
       float x[N];
@@ -249,13 +306,20 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
       for (int i = 0; i < N; i += 2) {
         float e0, e1;
         upk2(fma2(pk2(x[i], x[i + 1]), mul, sub), e0, e1);
-        part_sum = add2(part_sum, pk2(exp2_unit(e0), exp2_unit(e1)));
+        part_sum[(i >> 1) & 1] = add2(part_sum[(i >> 1) & 1], pk2(exp2_unit(e0), exp2_unit(e1)));
       }
     }
     float even, odd;
-    upk2(part_sum, even, odd);
+    upk2(add2(part_sum[0], part_sum[1]), even, odd);
     sum = sum * pow2_down(scale - now) + (even + odd);
     scale = now;
+  };
+  for (int t = 0; t < turns; t += 2) {   // two sets of registers: one on its way, one worked on
+    fetch(raw_b);
+    turn(raw_a, t);
+    if (t + 1 == turns) break;
+    fetch(raw_a);
+    turn(raw_b, t + 1);
   }
   m = fmaxf(m, last);
   const float now = sum_scale(m);
@@ -263,25 +327,16 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
   scale = now;
 
   // candidates: elements that reach the last bound (without turns there is none)
-  auto offer = [&](float v, int label) {
-    if (v >= bound && v > -INFINITY) {
-      const int at = atomicAdd(&sh.n, 1);
-      if (at < ROW_LIST) {
-        list.value[at] = v;
-        list.label[at] = label;
-      }
-    }
-  };
   __syncthreads();
   const int noted = sh.noted;
-  offer(first, tid);
-  offer(last, tail + tid);
+  offer_candidate(sh, bound, first, tid);
+  offer_candidate(sh, bound, last, tail + tid);
   for (int i = tid; i < min(noted, ROW_NOTED); i += ROW_NT) {
     float x[N];
     Vec<T>::get(list.vector[i], x);
     const int label = head + list.number[i] * N;
 #pragma unroll
-    for (int j = 0; j < N; ++j) offer(x[j], label + j);
+    for (int j = 0; j < N; ++j) offer_candidate(sh, bound, x[j], label + j);
   }
   // the segment's log-sum-exp
   float top = m, most = scale;
@@ -321,120 +376,117 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
     p.lse[out] = top == -INFINITY ? (total == 0.0 ? -INFINITY : NAN) : base + log(total) - excess;
   }
   Best* best = p.best + out * W;
-  if (noted <= ROW_NOTED && n <= ROW_LIST) {
-    for (int i = tid; i < max(n, W); i += ROW_NT) {
-      if (i >= n) {
-        best[i] = Best{-INFINITY, -1};
-        continue;
-      }
-      const float mine = list.value[i];
-      const int label = list.label[i];
-      int rank = 0;
-#pragma unroll 8
-      for (int j = 0; j < n; ++j) rank += before(list.value[j], list.label[j], mine, label);
-      if (rank < W) best[rank] = Best{mine, label};
-    }
-    return;
+  if (noted > ROW_NOTED || !rank_candidates(sh, n, W, best))
+    best_by_passes(sh, [&](int k) { return Best{to_f32<T>(z[k]), k}; }, from, to, W, best);
+}
+
+// A row's segments put together in the place of the first one: the sum of their shares of the log-sum-exp, and the W best of their
+// lists, by a bound from group maxima as in a segment.  What other blocks wrote is read past the L1.
+__device__ __forceinline__ Best load_best(const Best* p) {
+  const int2 v = __ldcg(reinterpret_cast<const int2*>(p));
+  return Best{__int_as_float(v.x), v.y};
+}
+__device__ __forceinline__ void merge_row(const RowParts& p, long long row, int W, SelectShared& sh) {
+  const int tid = threadIdx.x, entries = p.parts * W;
+  Best* best = p.best + row * entries;
+  double* parts = p.lse + row * p.parts;
+  constexpr int EACH = 4;
+  Best mine[EACH];
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) mine[i] = tid + i * ROW_NT < entries ? load_best(best + tid + i * ROW_NT) : Best{-INFINITY, -1};
+  if (tid == 0) sh.n = 0;
+  float head = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) head = fmaxf(head, mine[i].value);
+#pragma unroll 4
+  for (int e = tid + EACH * ROW_NT; e < entries; e += ROW_NT) head = fmaxf(head, load_best(best + e).value);
+  const float bound = group_bound(sh, head, W);
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) offer_candidate(sh, bound, mine[i].value, mine[i].label);
+#pragma unroll 4
+  for (int e = tid + EACH * ROW_NT; e < entries; e += ROW_NT) {
+    const Best b = load_best(best + e);
+    offer_candidate(sh, bound, b.value, b.label);
   }
-  Best before_it{INFINITY, -1};
-  for (int i = 0; i < W; ++i) {
-    Best b{-INFINITY, INT32_MAX};
-    for (int k = from + tid; k < to; k += ROW_NT) {
-      const float f = to_f32<T>(z[k]);
-      if (f > -INFINITY && before(before_it.value, before_it.label, f, k) && before(f, k, b.value, b.label)) b = Best{f, k};
+  if (tid < 32) {
+    double top = -INFINITY, sum = 0.0;
+    bool bad = false;
+    for (int j = tid; j < p.parts; j += 32) {
+      const double v = __ldcg(parts + j);
+      top = fmax(top, v);
+      bad = bad || isnan(v);
     }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const Best c{__shfl_xor_sync(0xffffffffu, b.value, o), __shfl_xor_sync(0xffffffffu, b.label, o)};
-      if (before(c.value, c.label, b.value, b.label)) b = c;
-    }
+    for (int o = 16; o > 0; o >>= 1) top = fmax(top, __shfl_xor_sync(0xffffffffu, top, o));
+    for (int j = tid; j < p.parts; j += 32) sum += (double)exp2_unit((float)(__ldcg(parts + j) - top) * LOG2E);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    bad = __any_sync(0xffffffffu, bad);
+    if (tid == 0) parts[0] = bad ? NAN : top + log(sum);
+  }
+  __syncthreads();                             // (all entries have been read, but for the passes below)
+  if (!rank_candidates(sh, sh.n, W, best)) {
+    // many equal ones: best of passes into shared memory first, as it takes the place of what the passes read
     __syncthreads();
-    if ((tid & 31) == 0) sh.best[tid >> 5] = b;
+    Best* found = reinterpret_cast<Best*>(sh.row.value);
+    best_by_passes(sh, [&](int k) { return load_best(best + k); }, 0, entries, W, found);
     __syncthreads();
-    for (int w = 0; w < ROW_NT / 32; ++w)
-      if (before(sh.best[w].value, sh.best[w].label, b.value, b.label)) b = sh.best[w];
-    if (tid == 0) best[i] = b.label == INT32_MAX ? Best{-INFINITY, -1} : b;   // (overflowed: there are more than W)
-    before_it = b;
+    if (tid < W) best[tid] = found[tid];
   }
 }
 
-// The W best proposals of an utterance from its segments' lists.  A proposal's score is score[w] + (z - lse + rho) in double; the
-// segments' shares of lse are put together first.  As for a segment a bound from group maxima (rounded down to fp32, so it errs
-// on the safe side) leaves few proposals to rank.  Every entry of the lists has a thread of its own where there are enough: a walk
-// down the lists took 20 us in dependent loads.
-__device__ __forceinline__ void merge_segments(const LmSelectArgs& a, const RowParts& p, int utterance, SelectShared& sh) {
+// The W best proposals of an utterance from its rows' lists.  A proposal's score is score[w] + (z - lse + rho) in double.  As for a
+// segment a bound from group maxima (rounded down to fp32, so it errs on the safe side) leaves few proposals to rank.
+__device__ __forceinline__ void merge_rows(const LmSelectArgs& a, const RowParts& p, int utterance, SelectShared& sh) {
   MergeShared& mg = sh.merge;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, W = a.W;
+  const int tid = threadIdx.x, W = a.W, entries = W * W;   // entry w W + j: place j of beam w
   const long long row0 = (long long)utterance * W;
-  // entry ((w parts + i) W + j): place j of segment i of beam w
-  const int per_beam = p.parts * W, entries = W * per_beam;
-  const Best* all = p.best + row0 * per_beam;
-  auto entry = [&](int e) {   // past the L1: other blocks wrote it
-    const int2 v = __ldcg(reinterpret_cast<const int2*>(all) + e);
-    return Best{__int_as_float(v.x), v.y};
-  };
-  const Best first = tid < entries ? entry(tid) : Best{-INFINITY, -1};     // on its way while the sums are put together
+  constexpr int EACH = MERGE_LIST / ROW_NT;
+  Best mine[EACH];
 #pragma unroll
-  for (int i = 0; i < MAX_BEAMS / (ROW_NT / 32); ++i) {
-    const int w = warp + i * (ROW_NT / 32);
-    if (w >= W) break;
-    const double* parts = p.lse + (row0 + w) * p.parts;
-    const float score = a.score[row0 + w];
-    const bool ended = a.done && a.done[row0 + w] && isfinite(score);
-    double lse = lane < p.parts ? __ldcg(parts + lane) : -INFINITY;         // (a beam that is empty or ended left none: not used)
-    if (p.parts > 1 && isfinite(score) && !ended) {
-      double top = lse;
-      bool bad = isnan(lse);
-      for (int j = lane + 32; j < p.parts; j += 32) {
-        top = fmax(top, __ldcg(parts + j));
-        bad = bad || isnan(__ldcg(parts + j));
-      }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) top = fmax(top, __shfl_xor_sync(0xffffffffu, top, o));
-      double sum = (double)exp2_unit((float)(lse - top) * LOG2E);
-      for (int j = lane + 32; j < p.parts; j += 32) sum += (double)exp2_unit((float)(__ldcg(parts + j) - top) * LOG2E);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      lse = __any_sync(0xffffffffu, bad) ? NAN : top + log(sum);
-    }
-    if (lane == 0) {
-      mg.score[w] = score;
-      mg.lse[w] = isfinite(score) && !ended && isfinite(lse) ? lse : NAN;   // (not finite: nothing but -inf, a NaN or +inf)
-      mg.ended[w] = ended;
-    }
+  for (int i = 0; i < EACH; ++i) {
+    const int e = tid + i * ROW_NT;
+    mine[i] = e < entries ? load_best(p.best + (row0 + e / W) * p.parts * W + e % W) : Best{-INFINITY, -1};
+  }
+  if (tid < W) {
+    const float score = a.score[row0 + tid];
+    const bool ended = a.done && a.done[row0 + tid] && isfinite(score);
+    const double lse = __ldcg(p.lse + (row0 + tid) * p.parts);              // (a beam that is empty or ended left none: not used)
+    mg.score[tid] = score;
+    mg.lse[tid] = isfinite(score) && !ended && isfinite(lse) ? lse : NAN;   // (not finite: nothing but -inf, a NaN or +inf)
+    mg.ended[tid] = ended;
   }
   if (tid == 0) sh.n = 0;
   __syncthreads();
   auto proposal = [&](int e, const Best& b) {
-    const int w = e / per_beam;
+    const int w = e / W;
     Proposal q{NO_PROPOSAL, -INFINITY, -1, w};
+    if (e >= entries) return q;
     if (mg.ended[w]) {
-      if (e == w * per_beam) q = Proposal{order_key(mg.score[w]), 0.0f, a.eos, w};
+      if (e == w * W) q = Proposal{order_key(mg.score[w]), 0.0f, a.eos, w};
     } else if (!isnan(mg.lse[w]) && b.label >= 0) {
       const double c = mg.score[w] + (((double)b.value - mg.lse[w]) + (double)a.rho);
       if (isfinite((float)c)) q = Proposal{order_key(c), b.value, b.label, w};
     }
     return q;
   };
-  Proposal mine{NO_PROPOSAL, -INFINITY, -1, 0};
-  if (tid < entries) mine = proposal(tid, first);
-  long long head = mine.key;
-  for (int e = tid + ROW_NT; e < entries; e += ROW_NT) head = max(head, proposal(e, entry(e)).key);
-  const float low = group_bound(sh, __double2float_rd(key_score(head)), W);
-  const long long bound = order_key((double)low);
-  auto offer = [&](const Proposal& q) {
-    if (q.key > NO_PROPOSAL && q.key >= bound) {
-      const int at = atomicAdd(&sh.n, 1);
-      if (at < MERGE_LIST) {
+  long long head = NO_PROPOSAL;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i)
+    if (i * ROW_NT < entries) head = max(head, proposal(tid + i * ROW_NT, mine[i]).key);
+  const long long bound = order_key((double)group_bound(sh, __double2float_rd(key_score(head)), W));
+#pragma unroll
+  for (int i = 0; i < EACH; ++i)
+    if (i * ROW_NT < entries) {
+      const Proposal q = proposal(tid + i * ROW_NT, mine[i]);
+      if (q.key > NO_PROPOSAL && q.key >= bound) {
+        const int at = atomicAdd(&sh.n, 1);
         mg.key[at] = q.key;
         mg.z[at] = q.z;
         mg.label[at] = q.label;
         mg.beam[at] = q.beam;
       }
     }
-  };
-  offer(mine);
-  for (int e = tid + ROW_NT; e < entries; e += ROW_NT) offer(proposal(e, entry(e)));
   __syncthreads();
   const int n = sh.n;
   auto store = [&](int i, const Proposal& q, bool some) {
@@ -445,50 +497,38 @@ __device__ __forceinline__ void merge_segments(const LmSelectArgs& a, const RowP
     if (a.done_out) a.done_out[o] = some && q.label == a.eos;
   };
   auto listed = [&](int i) { return Proposal{mg.key[i], mg.z[i], mg.label[i], mg.beam[i]}; };
-  if (n <= MERGE_LIST) {
-    for (int i = tid; i < max(n, W); i += ROW_NT) {
-      if (i >= n) {
-        store(i, Proposal{}, false);
-        continue;
-      }
-      const Proposal q = listed(i);
-      int rank = 0, equal = 0;
+  for (int i = tid; i < max(n, W); i += ROW_NT) {
+    if (i >= n) {
+      store(i, Proposal{}, false);
+      continue;
+    }
+    const Proposal q = listed(i);
+    int rank = 0, equal = 0;
 #pragma unroll 8
-      for (int j = 0; j < n; ++j) {
-        const long long k = mg.key[j];
-        rank += k > q.key;
-        equal += k == q.key;
-      }
-      if (rank < W && equal > 1)
-        for (int j = 0; j < n; ++j) rank += mg.key[j] == q.key && before(listed(j), q);
-      if (rank < W) store(rank, q, true);
+    for (int j = 0; j < n; ++j) {
+      const long long k = mg.key[j];
+      rank += k > q.key;
+      equal += k == q.key;
     }
-    return;
-  }
-  // more proposals at the bound than the list holds (equal beams of equal logits): one after the other
-  Proposal last{INT64_MAX, INFINITY, -1, -1};
-  for (int i = 0; i < W; ++i) {
-    Proposal b{NO_PROPOSAL, -INFINITY, INT32_MAX, INT32_MAX};
-    for (int e = tid; e < entries; e += ROW_NT) {
-      const Proposal q = proposal(e, entry(e));
-      if (q.key > NO_PROPOSAL && before(last, q) && before(q, b)) b = q;
-    }
-    __syncthreads();
-    mg.key[tid] = b.key;
-    mg.z[tid] = b.z;
-    mg.label[tid] = b.label;
-    mg.beam[tid] = b.beam;
-    __syncthreads();
-    for (int j = 0; j < ROW_NT; ++j)
-      if (before(listed(j), b)) b = listed(j);
-    if (tid == 0) store(i, b, true);                        // (overflowed: there are more than W)
-    last = b;
+    if (rank < W && equal > 1)
+      for (int j = 0; j < n; ++j) rank += mg.key[j] == q.key && before(listed(j), q);
+    if (rank < W) store(rank, q, true);
   }
 }
 
-// One block per segment; the last block of an utterance to be through its segment merges them all.  A block that arrives publishes
-// what its threads wrote (a barrier and a fence before the count), the last one reads the others' after the count and a fence, past
-// the L1.  The count wraps to 0 for the next call.
+// One block per segment; the last of a row's blocks to be through merges the row, the last of an utterance's rows the utterance.
+// A block that arrives publishes what its threads wrote (a barrier and a fence before the count), the last one reads the others' after
+// the count and a fence, past the L1.  The counts wrap to 0 for the next call.
+__device__ __forceinline__ bool last_to_arrive(uint32_t* count, uint32_t of, SelectShared& sh) {
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    __threadfence();
+    sh.last = atomicInc(count, of - 1) == of - 1;
+    __threadfence();
+  }
+  __syncthreads();
+  return sh.last != 0;
+}
 template <typename T>
 __global__ void __launch_bounds__(ROW_NT, ROW_BLOCKS) k_lm_select(const LmSelectArgs a, const RowParts p) {
   __shared__ __align__(16) SelectShared sh;
@@ -496,16 +536,13 @@ __global__ void __launch_bounds__(ROW_NT, ROW_BLOCKS) k_lm_select(const LmSelect
   const int part = blockIdx.x % p.parts, utterance = (int)(row / a.W);
   pdl_wait();
   pdl_trigger();   // (nothing of a later kernel starts to read or write before this grid has ended)
-  if (isfinite(a.score[row]) && !(a.done && a.done[row])) best_of_segment<T>(a, p, row, part, sh);
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    const uint32_t blocks = (uint32_t)a.W * p.parts;
-    __threadfence();
-    sh.last = atomicInc(a.arrived + utterance, blocks - 1) == blocks - 1;
-    __threadfence();
+  const bool live = isfinite(a.score[row]) && !(a.done && a.done[row]);
+  if (live) best_of_segment<T>(a, p, row, part, sh);
+  if (p.parts > 1) {
+    if (!last_to_arrive(a.arrived + a.B + row, p.parts, sh)) return;
+    if (live) merge_row(p, row, a.W, sh);
   }
-  __syncthreads();
-  if (sh.last) merge_segments(a, p, utterance, sh);
+  if (last_to_arrive(a.arrived + utterance, a.W, sh)) merge_rows(a, p, utterance, sh);
 }
 
 // Moves of up to Q4_REORDER_MAX tensors, cut into vectors of `width` bytes.
