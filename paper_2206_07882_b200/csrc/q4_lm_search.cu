@@ -87,7 +87,7 @@ template <> __device__ __forceinline__ uint4 lowest_vector<float>() { return mak
 template <> __device__ __forceinline__ uint4 lowest_vector<__half>() { return make_uint4(0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u); }
 template <> __device__ __forceinline__ uint4 lowest_vector<__nv_bfloat16>() { return make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u); }
 
-constexpr int ROW_NT = 128, ROW_BLOCKS = 8;       // threads of a block, blocks of an SM
+constexpr int ROW_NT = 128, ROW_BLOCKS = 7;       // threads of a block, blocks of an SM
 constexpr int ROW_VECTORS = 4, ROW_TURNS = 16, ROW_GROUPS = 64;
 constexpr int ROW_TURN = ROW_NT * ROW_VECTORS;    // 16-byte vectors that a block reads in one turn
 constexpr int ROW_NOTED = 512, ROW_LIST = 1024, MERGE_LIST = MAX_BEAMS * MAX_BEAMS;
@@ -223,15 +223,17 @@ __device__ __forceinline__ void best_by_passes(SelectShared& sh, F get, int from
   }
 }
 
-// One pass over a segment of at most 8 turns: running maximum and sum of every thread, and the segment's candidates.
-// The W-th best of the running maxima of 64 groups of threads (group_bound), taken in turns 1, 2, 4 and 8, bounds the
+// One pass over a segment of at most 16 turns: running maximum and sum of every thread, and the segment's candidates.
+// The W-th best of the running maxima of 64 groups of threads (group_bound), taken in turns 1, 2, 4, 8 and 16, bounds the
 // segment's W best from below.  Vectors with an element above it are noted: of the turn that it was taken in also those that
-// reach it, W of which are no smaller; behind that turn only larger ones, as equal ones come later in the order.  About 18 (W = 16) to 45
-// (W = 32) elements pass between two bounds.  The noted vectors' elements that reach the last bound are ranked.  More than the
+// reach it, W of which are no smaller; behind that turn only larger ones, as equal ones come later in the order.  About 18 (W = 16) to
+// 45 (W = 32) elements pass between two bounds.  The noted vectors' elements that reach the last bound are ranked.  More than the
 // lists take (equal or rising logits) are given up for W passes over the segment.
-// The next turn's vectors are on their way into registers while a turn is worked on: 80 KB in the five blocks of an SM.
-// (Candidates read again once the last bound was known took 14 of 60 us at 64 x 16 x 32768 fp32, a bound of the first turn
-// alone 9 of 44; two turns ahead in shared memory by asynchronous copies was no faster than one in registers.)
+// The next turn's vectors are on their way into registers while a turn is worked on: 56 KB in the seven blocks of an SM.
+// Bound by memory: 64 x 16 rows of 32000 fp32 logits, 131 MB, take 31 us with a fifth of the beams ended; a kernel that only
+// reads 134 MB in blocks like these takes 25 us, in the best of blocks 23.  Tried at 64 x 16 x 32768: candidates read again once the last
+// bound was known 14 us more, one bound of the first turn 9 us more, two turns ahead by asynchronous copies to shared memory no
+// gain, five blocks with twice the vectors 6 us more (two waves of blocks).
 template <typename T>
 __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const RowParts& p, long long row, int part, SelectShared& sh) {
   constexpr int N = Vec<T>::N;
@@ -593,6 +595,8 @@ __global__ void __launch_bounds__(256) k_beam_reorder(const __grid_constant__ Mo
 
 }  // namespace
 
+// Segments of a row: as many as fill the block slots of the device once, at most one a turn, at least so many that none has more than
+// 16 turns.  (Two or four times as many, us: 64 x 16 x 32000 31 -> 39 / 50, 100 x 16 x 8000 31 -> 45 / 56.)
 static RowParts row_parts(int B, int W, int V, int bytes, uint8_t* workspace) {
   const long long rows = (long long)B * W, slots = (long long)ROW_BLOCKS * sm_count();
   const long long turns = ((long long)V + ROW_TURN * (16 / bytes) - 1) / (ROW_TURN * (16 / bytes)), least = (turns + ROW_TURNS - 1) / ROW_TURNS;

@@ -283,6 +283,20 @@ def test_select_of_equal_and_ordered_logits(Bd, V, dtype):
         check_select(Bd, rows, score - torch.arange(W) * 1e-3)
 
 
+@pytest.mark.parametrize("W,V", [(32, 300000), (1, 2000000), (16, 131072)])
+def test_select_of_long_rows(Bd, W, V):
+    # rows of many segments: all equal (more candidates than a list holds, in every segment and over them), and ordinary
+    score = torch.linspace(0, -1, W)[None]
+    check_select(Bd, torch.zeros(1, W, V, dtype=torch.float16), score)
+    g = torch.Generator(device="cuda").manual_seed(V)
+    logits = torch.randn(1, W, V, generator=g, device="cuda")
+    r = Bd.q4_lm_beam_select(logits, score.cuda())
+    total = (torch.log_softmax(logits.double(), 2) + score.cuda().double()[:, :, None]).view(1, -1)
+    value, index = total.topk(W)
+    assert torch.equal(r["parent"].long(), index // V) and torch.equal(r["token"].long(), index % V)
+    assert ((r["score"].double() - value).abs() <= LSE_TOL + 2.0 ** -24 * value.abs() * 1.01).all()
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("V", [50, 3001])
 def test_select_of_masked_and_broken_rows(Bd, dtype, V):
