@@ -1895,7 +1895,7 @@ int q4_rmsnorm_quantize(const void* x, int64_t x_stride, const void* residual, i
   if (residual && ((sum_out == x && sum_stride != x_stride) || (sum_out == residual && sum_stride != residual_stride)))
     return Q4_ERR_UNSUPPORTED;
   if (k_pad % 32 != 0 || !aligned16(q_out) || !aligned_to(x, es) || !aligned_to(residual, es) || !aligned_to(sum_out, es) ||
-      !aligned_to(gain, 4) || !aligned_to(scale_out, 4))
+      !aligned16(gain) || !aligned_to(scale_out, 4))
     return Q4_ERR_ALIGN;
   if (rows == 0) return Q4_OK;
   NormArgs a;

@@ -3,6 +3,10 @@
 // With h the row (after the addition, rounded to its type) and v_i = h_i g_i:
 //   scale = max |v| / sqrt(mean h^2 + eps) / 127,  code_i = rne(127 v_i / max |v|).
 // Codes need the row's maximum, the scale its sum of squares as well; both come from one reduction.
+//
+// Codes are those of exact arithmetic.  In fp32 t = v (127 / max |v|) is off by at most four roundings, 127 * 4 * 2^-24 < 3.1e-5; an
+// element whose t lies further than that from a half is decided by it.  The others are decided in double, where v is exact
+// and a half is met exactly (`settle`); the maximum is then taken from the exact products too.
 #include <cuda_bf16.h>
 
 #include "q4_internal.h"
@@ -20,61 +24,345 @@ template <> __device__ __forceinline__ float from_f32(float v) { return v; }
 template <> __device__ __forceinline__ __half from_f32(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32(float v) { return __float2bfloat16_rn(v); }
 
-// One block per row, all in double: v = h g has at most 48 bits, so products are exact.
+// 16 bytes of a row
 template <typename T>
-__global__ void __launch_bounds__(256) k_rmsnorm_quantize(const NormArgs a) {
-  __shared__ double s_sum[8], s_max[8];
-  const T* gain_row = nullptr;
-  (void)gain_row;
-  for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const T* x = static_cast<const T*>(a.x) + row * a.x_ld;
-    const T* r = a.residual ? static_cast<const T*>(a.residual) + row * a.r_ld : nullptr;
-    T* h = a.sum ? static_cast<T*>(a.sum) + row * a.s_ld : nullptr;
-    auto value = [&](int i) {   // h_i; the thread that stores element i is the one that reads it again
-      return to_f32<T>(r ? h[i] : x[i]);
-    };
-    if (r)
-      for (int i = threadIdx.x; i < a.k; i += 256) h[i] = from_f32<T>(__fadd_rn(to_f32<T>(x[i]), to_f32<T>(r[i])));
-    double sum = 0.0, top = 0.0;
-    bool bad = false;
-    for (int i = threadIdx.x; i < a.k; i += 256) {
-      const float f = value(i);
-      const double v = fabs((double)f * (double)a.gain[i]);
-      sum += (double)f * (double)f;
-      bad = bad || !(v <= 1.7e308) || !(fabsf(f) <= 3.4028235e38f);
-      top = fmax(top, v);
+union Vec {
+  static constexpr int N = 16 / (int)sizeof(T);
+  uint4 v16;
+  uint2 v8[2];
+  uint32_t v4[4];
+  T e[N];
+  __device__ Vec() {}
+};
+// `width`: bytes of a load that the rows' alignment allows; n < N: the elements that there are (the others become 0)
+template <typename T>
+__device__ __forceinline__ void load_vec(Vec<T>& v, const T* p, int n, int width) {
+  constexpr int N = Vec<T>::N;
+  if (n >= N && width == 16) {
+    v.v16 = *reinterpret_cast<const uint4*>(p);
+  } else if (n >= N && width == 8) {
+    v.v8[0] = reinterpret_cast<const uint2*>(p)[0];
+    v.v8[1] = reinterpret_cast<const uint2*>(p)[1];
+  } else if (n >= N && width == 4) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v.v4[i] = reinterpret_cast<const uint32_t*>(p)[i];
+  } else {
+    v.v16 = make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i < n) v.e[i] = p[i];
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store_vec(const Vec<T>& v, T* p, int n, int width) {
+  constexpr int N = Vec<T>::N;
+  if (n >= N && width == 16) {
+    *reinterpret_cast<uint4*>(p) = v.v16;
+  } else if (n >= N && width == 8) {
+    reinterpret_cast<uint2*>(p)[0] = v.v8[0];
+    reinterpret_cast<uint2*>(p)[1] = v.v8[1];
+  } else if (n >= N && width == 4) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) reinterpret_cast<uint32_t*>(p)[i] = v.v4[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i < n) p[i] = v.e[i];
+  }
+}
+// gains of elements [at, at + N) (at a multiple of N, gain 16-byte aligned); 0 behind the last
+template <int N>
+__device__ __forceinline__ void load_gain(float (&g)[N], const float* gain, int at, int k) {
+  if (at + N <= k) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const float4 f = __ldg(reinterpret_cast<const float4*>(gain + at + i));
+      g[i] = f.x;
+      g[i + 1] = f.y;
+      g[i + 2] = f.z;
+      g[i + 3] = f.w;
     }
-    for (int o = 16; o > 0; o >>= 1) {
-      sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      top = fmax(top, __shfl_xor_sync(0xffffffffu, top, o));
-    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) g[i] = at + i < k ? __ldg(gain + at + i) : 0.0f;
+  }
+}
+// N codes given as integers in fp32, one byte each
+template <int N>
+__device__ __forceinline__ void store_codes(int8_t* q, const int (&c)[N]) {
+  uint32_t w[N / 4];
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i)
+    w[i] = __byte_perm(__byte_perm(c[4 * i], c[4 * i + 1], 0x0040), __byte_perm(c[4 * i + 2], c[4 * i + 3], 0x0040), 0x5410);
+  if (N == 8)
+    *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[N / 4 - 1]);
+  else
+    *reinterpret_cast<uint32_t*>(q) = w[0];
+}
+
+// Sum and maximum over the THREADS threads of a row, the same in all of them.
+template <int THREADS, typename F>
+__device__ __forceinline__ void row_reduce(F& sum, F& top, F (*s)[2]) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+  }
+  if (THREADS > 32) {
     if ((threadIdx.x & 31) == 0) {
-      s_sum[threadIdx.x >> 5] = sum;
-      s_max[threadIdx.x >> 5] = top;
+      s[threadIdx.x >> 5][0] = sum;
+      s[threadIdx.x >> 5][1] = top;
     }
-    bad = __syncthreads_or(bad) != 0;
-    sum = top = 0.0;
-    for (int w = 0; w < 8; ++w) {
-      sum += s_sum[w];
-      top = fmax(top, s_max[w]);
+    __syncthreads();
+    sum = top = F(0);
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) {
+      sum += s[w][0];
+      top = max(top, s[w][1]);
     }
-    int8_t* q = a.q + row * a.k_pad;
-    for (int i = threadIdx.x; i < a.k_pad; i += 256)
-      q[i] = i < a.k && !bad && top > 0.0 ? (int8_t)__double2int_rn(127.0 * ((double)value(i) * (double)a.gain[i]) / top) : (int8_t)0;
-    if (threadIdx.x == 0)
-      a.scale[row] = bad ? __int_as_float(0x7fffffff) : (float)((top > 0.0 ? top / sqrt(sum / a.k + (double)a.eps) : 1.0) / 127.0);
     __syncthreads();
   }
+}
+template <int THREADS>
+__device__ __forceinline__ bool row_any(bool v) {
+  return THREADS > 32 ? __syncthreads_or(v) != 0 : __any_sync(0xffffffffu, v) != 0;
+}
+
+// A row in double, from memory: for rows that hold no more than zeros, a NaN or infinity, or values whose squares or products leave
+// the range of fp32, and for rows too long for registers.  Elements vec, vec + THREADS, ... of N are thread `t`'s, as everywhere.
+template <typename T, int THREADS>
+__device__ __noinline__ void norm_row(const NormArgs& a, long long row, int t, double (*s)[2]) {
+  constexpr int N = Vec<T>::N;
+  const T* h = a.sum ? static_cast<const T*>(a.sum) + row * a.s_ld : static_cast<const T*>(a.x) + row * a.x_ld;
+  int8_t* q = a.q + row * a.k_pad;
+  double sum = 0.0, top = 0.0;
+  bool bad = false;
+  for (int v = t; v * N < a.k; v += THREADS)
+    for (int i = v * N; i < min(v * N + N, a.k); ++i) {
+      const double f = to_f32<T>(h[i]), p = fabs(f * (double)a.gain[i]);
+      sum += f * f;
+      top = fmax(top, p);
+      bad = bad || !(fabs(f) <= 3.5e38) || !(p <= 1e300);
+    }
+  bad = row_any<THREADS>(bad);
+  row_reduce<THREADS>(sum, top, s);
+  for (int v = t; v * N < a.k_pad; v += THREADS) {
+    int c[N];
+    for (int i = 0; i < N; ++i) {
+      const int at = v * N + i;
+      c[i] = at < a.k && !bad && top > 0.0 ? __double2int_rn(127.0 * ((double)to_f32<T>(h[at]) * (double)a.gain[at]) / top) : 0;
+    }
+    store_codes<N>(q + v * N, c);
+  }
+  if (t == 0) a.scale[row] = bad ? __int_as_float(0x7fffffff) : (float)((top > 0.0 ? top / sqrt(sum / a.k + (double)a.eps) : 1.0) / 127.0);
+}
+
+constexpr float MAGIC = 12582912.0f;   // 1.5 * 2^23: adding it leaves the nearest integer in the low bits
+constexpr float SETTLED = 0.5f - 3.2e-5f;
+
+__device__ __forceinline__ uint4 load_once(const void* p) {   // past the L1, which keeps the gains
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+template <typename T>
+__device__ __forceinline__ void unpack(const Vec<T>& v, float (&f)[Vec<T>::N]) {
+#pragma unroll
+  for (int i = 0; i < Vec<T>::N; ++i) f[i] = to_f32<T>(v.e[i]);
+}
+template <>
+__device__ __forceinline__ void unpack<__nv_bfloat16>(const Vec<__nv_bfloat16>& v, float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = __uint_as_float(v.v4[i] << 16);
+    f[2 * i + 1] = __uint_as_float(v.v4[i] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ void pack(Vec<float>& v, const float (&f)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v.e[i] = f[i];
+}
+__device__ __forceinline__ void pack(Vec<__half>& v, const float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __half2 p = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+    v.v4[i] = *reinterpret_cast<const uint32_t*>(&p);
+  }
+}
+__device__ __forceinline__ void pack(Vec<__nv_bfloat16>& v, const float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+    v.v4[i] = *reinterpret_cast<const uint32_t*>(&p);
+  }
+}
+
+// A row per group of THREADS threads, 128 or THREADS threads a block; everything is read and written once, the products v lie in
+// registers, NV vectors of 16 bytes of the row a thread.  WHOLE: rows are 16-byte aligned and a multiple of that long.
+// Bound by memory.  One warp a row needs no barrier; wider groups take rows that a warp's registers do not hold, and few rows,
+// where a row's latency is the call's.
+__host__ __device__ constexpr int norm_blocks(int threads, int nv) { return threads > 128 ? (nv <= 2 ? 2 : 1) : nv <= 2 ? 8 : nv <= 4 ? 6 : nv <= 6 ? 5 : 4; }
+template <typename T, int THREADS, int NV, bool WHOLE>
+__global__ void __launch_bounds__(THREADS > 128 ? THREADS : 128, norm_blocks(THREADS, NV)) k_rmsnorm_quantize(const NormArgs a, const int width) {
+  constexpr int N = Vec<T>::N, ROWS = THREADS >= 128 ? 1 : 128 / THREADS;
+  __shared__ float s_part[THREADS / 32][2];
+  __shared__ double s_part64[THREADS / 32][2];
+  const int t = threadIdx.x % THREADS;
+  pdl_wait();
+  pdl_trigger();
+  for (long long row = (long long)blockIdx.x * ROWS + threadIdx.x / THREADS; row < a.rows; row += (long long)gridDim.x * ROWS) {
+    const T* x = static_cast<const T*>(a.x) + row * a.x_ld;
+    const T* h = x;
+    int8_t* q = a.q + row * a.k_pad;
+    auto load = [&](Vec<T>& v, const T* p, int at) {
+      if (!WHOLE)
+        load_vec<T>(v, p + at, a.k - at, width);
+      else
+        v.v16 = at < a.k ? load_once(p + at) : make_uint4(0, 0, 0, 0);
+    };
+    Vec<T> raw[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) load(raw[j], x, (t + j * THREADS) * N);
+    if (a.residual) {
+      const T* r = static_cast<const T*>(a.residual) + row * a.r_ld;
+      T* out = static_cast<T*>(a.sum) + row * a.s_ld;
+      Vec<T> add[NV];
+#pragma unroll
+      for (int j = 0; j < NV; ++j) load(add[j], r, (t + j * THREADS) * N);
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int at = (t + j * THREADS) * N;
+        float f[N], g[N];
+        unpack<T>(raw[j], f);
+        unpack<T>(add[j], g);
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = __fadd_rn(f[i], g[i]);
+        pack(raw[j], f);
+        if (!WHOLE)
+          store_vec<T>(raw[j], out + at, a.k - at, width);
+        else if (at < a.k)
+          *reinterpret_cast<uint4*>(out + at) = raw[j].v16;
+      }
+      h = out;
+    }
+    float v[NV][N], sum = 0.0f, top = 0.0f;
+    {
+      uint64_t squares = pk2(0.0f, 0.0f);
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        float g[N], f[N];
+        load_gain<N>(g, a.gain, (t + j * THREADS) * N, a.k);
+        unpack<T>(raw[j], f);
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+          const uint64_t f2 = pk2(f[i], f[i + 1]);
+          squares = fma2(f2, f2, squares);
+          upk2(mul2(f2, pk2(g[i], g[i + 1])), v[j][i], v[j][i + 1]);
+          top = fmaxf(fmaxf(top, fabsf(v[j][i])), fabsf(v[j][i + 1]));
+        }
+      }
+      float odd;
+      upk2(squares, sum, odd);
+      sum += odd;
+    }
+    row_reduce<THREADS>(sum, top, s_part);
+    if (!(top > 1e-30f && top < 1e37f && sum > 1e-30f && sum < 1e38f)) {   // (a NaN or infinity is in the sum)
+      norm_row<T, THREADS>(a, row, t, s_part64);
+      continue;
+    }
+    if (t == 0) a.scale[row] = __fdiv_rn(__fdiv_rn(top, __fsqrt_rn(__fadd_rn(__fdiv_rn(sum, (float)a.k), a.eps))), 127.0f);
+    const float inv = __fdiv_rn(127.0f, top);
+    uint32_t unsettled = 0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int at = (t + j * THREADS) * N;
+      int c[N];
+      float off = 0.0f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float u = __fmul_rn(v[j][i], inv), m = __fadd_rn(u, MAGIC);
+        off = fmaxf(off, fabsf(__fsub_rn(u, __fsub_rn(m, MAGIC))));
+        c[i] = __float_as_int(m);
+      }
+      if (at < a.k_pad) store_codes<N>(q + at, c);
+      if (off > SETTLED) unsettled |= 1u << j;
+    }
+    if (!row_any<THREADS>(unsettled != 0)) continue;
+    double exact = 0.0, unused = 0.0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (fabsf(v[j][i]) == top) {
+          const int at = (t + j * THREADS) * N + i;
+          exact = fmax(exact, fabs((double)to_f32<T>(h[at]) * (double)a.gain[at]));
+        }
+    row_reduce<THREADS>(unused, exact, s_part64);
+#pragma unroll 1
+    for (int j = 0; j < NV; ++j) {
+      if (!(unsettled >> j & 1)) continue;
+      for (int i = 0; i < N; ++i) {
+        const int at = (t + j * THREADS) * N + i;
+        if (at >= a.k) break;
+        const float f = to_f32<T>(h[at]), g = a.gain[at], u = __fmul_rn(__fmul_rn(f, g), inv), m = __fadd_rn(u, MAGIC);
+        if (fabsf(__fsub_rn(u, __fsub_rn(m, MAGIC))) > SETTLED) q[at] = (int8_t)__double2int_rn(127.0 * ((double)f * (double)g) / exact);
+      }
+    }
+  }
+}
+
+// Rows of any length, from memory in double.
+template <typename T>
+__global__ void __launch_bounds__(512) k_rmsnorm_quantize_long(const NormArgs a) {
+  __shared__ double s_part64[16][2];
+  pdl_wait();
+  pdl_trigger();
+  for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    if (a.residual) {
+      constexpr int N = Vec<T>::N;
+      const T *x = static_cast<const T*>(a.x) + row * a.x_ld, *r = static_cast<const T*>(a.residual) + row * a.r_ld;
+      T* out = static_cast<T*>(a.sum) + row * a.s_ld;
+      for (int v = threadIdx.x; v * N < a.k; v += 512)
+        for (int i = v * N; i < min(v * N + N, a.k); ++i) out[i] = from_f32<T>(__fadd_rn(to_f32<T>(x[i]), to_f32<T>(r[i])));
+    }
+    norm_row<T, 512>(a, row, threadIdx.x, s_part64);
+  }
+}
+
+template <typename T, int THREADS, int NV>
+cudaError_t launch_rows(const NormArgs& a, int width, cudaStream_t s) {
+  constexpr int ROWS = THREADS >= 128 ? 1 : 128 / THREADS;
+  const long long blocks = (a.rows + ROWS - 1) / ROWS;
+  return launch_ex(width == 16 && a.k % Vec<T>::N == 0 ? k_rmsnorm_quantize<T, THREADS, NV, true> : k_rmsnorm_quantize<T, THREADS, NV, false>,
+                   dim3((unsigned)(blocks < (1 << 20) ? blocks : 1 << 20)), dim3(THREADS > 128 ? THREADS : 128), 0, s, true, 1, a, width);
+}
+template <typename T>
+cudaError_t launch_norm(const NormArgs& a, cudaStream_t s) {
+  // the widest load that every row of x, residual and sum allows
+  uintptr_t low = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.residual) | reinterpret_cast<uintptr_t>(a.sum);
+  if (a.rows > 1) low |= (uintptr_t)(a.x_ld | a.r_ld | a.s_ld) * sizeof(T);
+  const int width = low % 16 == 0 ? 16 : low % 8 == 0 ? 8 : low % 4 == 0 ? 4 : 2;
+  const int vectors = a.k_pad / Vec<T>::N;
+  // Many rows: the narrowest group that holds a row.  Few (less than 16 for each SM): no more than two vectors a thread.
+  if (a.rows >= 16LL * sm_count()) {
+    if (vectors <= 32 * 2) return launch_rows<T, 32, 2>(a, width, s);
+    if (vectors <= 32 * 4) return launch_rows<T, 32, 4>(a, width, s);
+    if (vectors <= 32 * 6) return launch_rows<T, 32, 6>(a, width, s);
+    if (vectors <= 32 * 8) return launch_rows<T, 32, 8>(a, width, s);
+    if (vectors <= 128 * 4) return launch_rows<T, 128, 4>(a, width, s);
+  }
+  if (vectors <= 128 * 2) return launch_rows<T, 128, 2>(a, width, s);
+  if (vectors <= 512 * 2) return launch_rows<T, 512, 2>(a, width, s);
+  if (vectors <= 512 * 4) return launch_rows<T, 512, 4>(a, width, s);
+  if (vectors <= 512 * 8) return launch_rows<T, 512, 8>(a, width, s);
+  return launch_ex(k_rmsnorm_quantize_long<T>, dim3((unsigned)(a.rows < (1 << 20) ? a.rows : 1 << 20)), dim3(512), 0, s, true, 1, a);
 }
 
 }  // namespace
 
 cudaError_t launch_rmsnorm_quantize(const NormArgs& a, int dtype, cudaStream_t s) {
-  const unsigned blocks = (unsigned)(a.rows < (1 << 20) ? a.rows : (1 << 20));
   timing_begin(s);
-  const cudaError_t e = dtype == Q4_F32   ? launch_ex(k_rmsnorm_quantize<float>, dim3(blocks), dim3(256), 0, s, false, 1, a)
-                        : dtype == Q4_F16 ? launch_ex(k_rmsnorm_quantize<__half>, dim3(blocks), dim3(256), 0, s, false, 1, a)
-                                          : launch_ex(k_rmsnorm_quantize<__nv_bfloat16>, dim3(blocks), dim3(256), 0, s, false, 1, a);
+  const cudaError_t e = dtype == Q4_F32 ? launch_norm<float>(a, s) : dtype == Q4_F16 ? launch_norm<__half>(a, s) : launch_norm<__nv_bfloat16>(a, s);
   timing_end(s);
   ++g_launches;
   return e != cudaSuccess ? e : cudaGetLastError();
