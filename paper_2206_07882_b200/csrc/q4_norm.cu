@@ -34,40 +34,71 @@ union Vec {
   T e[N];
   __device__ Vec() {}
 };
-// `width`: bytes of a load that the rows' alignment allows; n < N: the elements that there are (the others become 0)
+// Rows that are not 16-byte aligned.  The 16 bytes of a vector lie across two aligned granules, `shift` bytes into the first (the
+// same for all vectors of a row): both are read and put together.  A granule is read as a whole only where it lies inside
+// [lo, hi), the tensor's first and last byte; else the vector's elements are read one by one.  Elements from n on become 0.
+__device__ __forceinline__ uint4 across(const uint4& a, const uint4& b, int shift) {   // bytes [shift, shift + 16) of (a, b)
+  const int bits = (shift & 3) * 8;
+  switch (shift >> 2) {
+    case 0:
+      return make_uint4(__funnelshift_r(a.x, a.y, bits), __funnelshift_r(a.y, a.z, bits), __funnelshift_r(a.z, a.w, bits), __funnelshift_r(a.w, b.x, bits));
+    case 1:
+      return make_uint4(__funnelshift_r(a.y, a.z, bits), __funnelshift_r(a.z, a.w, bits), __funnelshift_r(a.w, b.x, bits), __funnelshift_r(b.x, b.y, bits));
+    case 2:
+      return make_uint4(__funnelshift_r(a.z, a.w, bits), __funnelshift_r(a.w, b.x, bits), __funnelshift_r(b.x, b.y, bits), __funnelshift_r(b.y, b.z, bits));
+    default:
+      return make_uint4(__funnelshift_r(a.w, b.x, bits), __funnelshift_r(b.x, b.y, bits), __funnelshift_r(b.y, b.z, bits), __funnelshift_r(b.z, b.w, bits));
+  }
+}
 template <typename T>
-__device__ __forceinline__ void load_vec(Vec<T>& v, const T* p, int n, int width) {
+__device__ __forceinline__ void load_across(Vec<T>& v, const T* p, int n, uintptr_t lo, uintptr_t hi) {
   constexpr int N = Vec<T>::N;
-  if (n >= N && width == 16) {
-    v.v16 = *reinterpret_cast<const uint4*>(p);
-  } else if (n >= N && width == 8) {
-    v.v8[0] = reinterpret_cast<const uint2*>(p)[0];
-    v.v8[1] = reinterpret_cast<const uint2*>(p)[1];
-  } else if (n >= N && width == 4) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p), granule = at & ~(uintptr_t)15;
+  v.v16 = make_uint4(0, 0, 0, 0);
+  if (n <= 0) return;
+  if (granule >= lo && granule + 32 <= hi) {
+    const uint4* g = reinterpret_cast<const uint4*>(granule);
+    v.v16 = across(g[0], g[1], (int)(at & 15));
+    if (n < N) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v.v4[i] = reinterpret_cast<const uint32_t*>(p)[i];
+      for (int i = 1; i < N; ++i)
+        if (i >= n) v.e[i] = T(0.0f);
+    }
   } else {
-    v.v16 = make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int i = 0; i < N; ++i)
       if (i < n) v.e[i] = p[i];
   }
 }
+// By whole warps, lane l holding the l-th of neighbouring vectors: a lane stores the granule that its vector and its neighbour's lie
+// in; the ends of what the warp holds are stored element by element.
 template <typename T>
-__device__ __forceinline__ void store_vec(const Vec<T>& v, T* p, int n, int width) {
+__device__ __forceinline__ void store_across(const Vec<T>& v, T* p, int n) {
   constexpr int N = Vec<T>::N;
-  if (n >= N && width == 16) {
-    *reinterpret_cast<uint4*>(p) = v.v16;
-  } else if (n >= N && width == 8) {
-    reinterpret_cast<uint2*>(p)[0] = v.v8[0];
-    reinterpret_cast<uint2*>(p)[1] = v.v8[1];
-  } else if (n >= N && width == 4) {
+  const int lane = threadIdx.x & 31, shift = (int)(reinterpret_cast<uintptr_t>(p) & 15);
+  const bool full = n >= N;
+  if (shift == 0) {                                            // the same for the whole warp
+    if (full) {
+      *reinterpret_cast<uint4*>(p) = v.v16;
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) reinterpret_cast<uint32_t*>(p)[i] = v.v4[i];
-  } else {
+      for (int i = 0; i < N; ++i)
+        if (i < n) p[i] = v.e[i];
+    }
+    return;
+  }
+  uint4 before;
+  before.x = __shfl_up_sync(0xffffffffu, v.v16.x, 1);
+  before.y = __shfl_up_sync(0xffffffffu, v.v16.y, 1);
+  before.z = __shfl_up_sync(0xffffffffu, v.v16.z, 1);
+  before.w = __shfl_up_sync(0xffffffffu, v.v16.w, 1);
+  const bool next_full = __shfl_down_sync(0xffffffffu, full, 1) && lane < 31;
+  const int in_front = (16 - shift) / (int)sizeof(T);          // elements of the vector in its first granule
+  if (full && lane > 0) *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(p) - shift) = across(before, v.v16, 16 - shift);
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (i < n) p[i] = v.e[i];
+  for (int i = 0; i < N; ++i) {
+    const bool alone = full ? (i < in_front ? lane == 0 : !next_full) : i < n;
+    if (alone) p[i] = v.e[i];
   }
 }
 // gains of elements [at, at + N) (at a multiple of N, gain 16-byte aligned); 0 behind the last
@@ -201,34 +232,39 @@ __device__ __forceinline__ void pack(Vec<__nv_bfloat16>& v, const float (&f)[8])
 // registers, NV vectors of 16 bytes of the row a thread.  WHOLE: rows are 16-byte aligned and a multiple of that long.
 // Bound by memory.  One warp a row needs no barrier; wider groups take rows that a warp's registers do not hold, and few rows,
 // where a row's latency is the call's.
-__host__ __device__ constexpr int norm_blocks(int threads, int nv) { return threads > 128 ? (nv <= 2 ? 2 : 1) : nv <= 2 ? 8 : nv <= 4 ? 6 : nv <= 6 ? 5 : 4; }
+// blocks of an SM: 64 registers a thread for up to 16 elements, 80 for up to 32, 96 and 128 for up to 48 and 64
+__host__ __device__ constexpr int norm_blocks(int threads, int elements) {
+  return 128 * (elements <= 16 ? 8 : elements <= 32 ? 6 : elements <= 48 ? 5 : 4) / (threads > 128 ? threads : 128);
+}
 template <typename T, int THREADS, int NV, bool WHOLE>
-__global__ void __launch_bounds__(THREADS > 128 ? THREADS : 128, norm_blocks(THREADS, NV)) k_rmsnorm_quantize(const NormArgs a, const int width) {
+__global__ void __launch_bounds__(THREADS > 128 ? THREADS : 128, norm_blocks(THREADS, NV * (16 / (int)sizeof(T)))) k_rmsnorm_quantize(const __grid_constant__ NormArgs a) {
   constexpr int N = Vec<T>::N, ROWS = THREADS >= 128 ? 1 : 128 / THREADS;
   __shared__ float s_part[THREADS / 32][2];
   __shared__ double s_part64[THREADS / 32][2];
   const int t = threadIdx.x % THREADS;
+  const uintptr_t lo_x = reinterpret_cast<uintptr_t>(a.x), hi_x = lo_x + ((a.rows - 1) * a.x_ld + a.k) * sizeof(T);
+  const uintptr_t lo_r = reinterpret_cast<uintptr_t>(a.residual), hi_r = lo_r + ((a.rows - 1) * a.r_ld + a.k) * sizeof(T);
   pdl_wait();
   pdl_trigger();
   for (long long row = (long long)blockIdx.x * ROWS + threadIdx.x / THREADS; row < a.rows; row += (long long)gridDim.x * ROWS) {
     const T* x = static_cast<const T*>(a.x) + row * a.x_ld;
     const T* h = x;
     int8_t* q = a.q + row * a.k_pad;
-    auto load = [&](Vec<T>& v, const T* p, int at) {
+    auto load = [&](Vec<T>& v, const T* p, int at, uintptr_t lo, uintptr_t hi) {
       if (!WHOLE)
-        load_vec<T>(v, p + at, a.k - at, width);
+        load_across<T>(v, p + at, a.k - at, lo, hi);
       else
         v.v16 = at < a.k ? load_once(p + at) : make_uint4(0, 0, 0, 0);
     };
     Vec<T> raw[NV];
 #pragma unroll
-    for (int j = 0; j < NV; ++j) load(raw[j], x, (t + j * THREADS) * N);
+    for (int j = 0; j < NV; ++j) load(raw[j], x, (t + j * THREADS) * N, lo_x, hi_x);
     if (a.residual) {
       const T* r = static_cast<const T*>(a.residual) + row * a.r_ld;
       T* out = static_cast<T*>(a.sum) + row * a.s_ld;
       Vec<T> add[NV];
 #pragma unroll
-      for (int j = 0; j < NV; ++j) load(add[j], r, (t + j * THREADS) * N);
+      for (int j = 0; j < NV; ++j) load(add[j], r, (t + j * THREADS) * N, lo_r, hi_r);
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         const int at = (t + j * THREADS) * N;
@@ -239,7 +275,7 @@ __global__ void __launch_bounds__(THREADS > 128 ? THREADS : 128, norm_blocks(THR
         for (int i = 0; i < N; ++i) f[i] = __fadd_rn(f[i], g[i]);
         pack(raw[j], f);
         if (!WHOLE)
-          store_vec<T>(raw[j], out + at, a.k - at, width);
+          store_across<T>(raw[j], out + at, a.k - at);
         else if (at < a.k)
           *reinterpret_cast<uint4*>(out + at) = raw[j].v16;
       }
@@ -313,7 +349,7 @@ __global__ void __launch_bounds__(THREADS > 128 ? THREADS : 128, norm_blocks(THR
 
 // Rows of any length, from memory in double.
 template <typename T>
-__global__ void __launch_bounds__(512) k_rmsnorm_quantize_long(const NormArgs a) {
+__global__ void __launch_bounds__(512) k_rmsnorm_quantize_long(const __grid_constant__ NormArgs a) {
   __shared__ double s_part64[16][2];
   pdl_wait();
   pdl_trigger();
@@ -330,31 +366,33 @@ __global__ void __launch_bounds__(512) k_rmsnorm_quantize_long(const NormArgs a)
 }
 
 template <typename T, int THREADS, int NV>
-cudaError_t launch_rows(const NormArgs& a, int width, cudaStream_t s) {
+cudaError_t launch_rows(const NormArgs& a, bool whole, cudaStream_t s) {
   constexpr int ROWS = THREADS >= 128 ? 1 : 128 / THREADS;
   const long long blocks = (a.rows + ROWS - 1) / ROWS;
-  return launch_ex(width == 16 && a.k % Vec<T>::N == 0 ? k_rmsnorm_quantize<T, THREADS, NV, true> : k_rmsnorm_quantize<T, THREADS, NV, false>,
-                   dim3((unsigned)(blocks < (1 << 20) ? blocks : 1 << 20)), dim3(THREADS > 128 ? THREADS : 128), 0, s, true, 1, a, width);
+  return launch_ex(whole ? k_rmsnorm_quantize<T, THREADS, NV, true> : k_rmsnorm_quantize<T, THREADS, NV, false>,
+                   dim3((unsigned)(blocks < (1 << 20) ? blocks : 1 << 20)), dim3(THREADS > 128 ? THREADS : 128), 0, s, true, 1, a);
 }
 template <typename T>
 cudaError_t launch_norm(const NormArgs& a, cudaStream_t s) {
-  // the widest load that every row of x, residual and sum allows
-  uintptr_t low = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.residual) | reinterpret_cast<uintptr_t>(a.sum);
+  // rows of x, residual and sum that are multiples of 16 bytes long and apart
+  uintptr_t low = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.residual) | reinterpret_cast<uintptr_t>(a.sum) | a.k * sizeof(T);
   if (a.rows > 1) low |= (uintptr_t)(a.x_ld | a.r_ld | a.s_ld) * sizeof(T);
-  const int width = low % 16 == 0 ? 16 : low % 8 == 0 ? 8 : low % 4 == 0 ? 4 : 2;
+  const bool whole = low % 16 == 0;
   const int vectors = a.k_pad / Vec<T>::N;
+  constexpr int MOST = 32 / Vec<T>::N;      // vectors of a thread in wide groups: 32 elements in registers
   // Many rows: the narrowest group that holds a row.  Few (less than 16 for each SM): no more than two vectors a thread.
   if (a.rows >= 16LL * sm_count()) {
-    if (vectors <= 32 * 2) return launch_rows<T, 32, 2>(a, width, s);
-    if (vectors <= 32 * 4) return launch_rows<T, 32, 4>(a, width, s);
-    if (vectors <= 32 * 6) return launch_rows<T, 32, 6>(a, width, s);
-    if (vectors <= 32 * 8) return launch_rows<T, 32, 8>(a, width, s);
-    if (vectors <= 128 * 4) return launch_rows<T, 128, 4>(a, width, s);
+    if (vectors <= 32 * 2) return launch_rows<T, 32, 2>(a, whole, s);
+    if (vectors <= 32 * 4) return launch_rows<T, 32, 4>(a, whole, s);
+    if (vectors <= 32 * 6) return launch_rows<T, 32, 6>(a, whole, s);
+    if (vectors <= 32 * 8) return launch_rows<T, 32, 8>(a, whole, s);
+    if (vectors <= 128 * MOST) return launch_rows<T, 128, MOST>(a, whole, s);
+    if (vectors <= 256 * MOST) return launch_rows<T, 256, MOST>(a, whole, s);
   }
-  if (vectors <= 128 * 2) return launch_rows<T, 128, 2>(a, width, s);
-  if (vectors <= 512 * 2) return launch_rows<T, 512, 2>(a, width, s);
-  if (vectors <= 512 * 4) return launch_rows<T, 512, 4>(a, width, s);
-  if (vectors <= 512 * 8) return launch_rows<T, 512, 8>(a, width, s);
+  if (vectors <= 128 * 2) return launch_rows<T, 128, 2>(a, whole, s);
+  if (vectors <= 512 * 2) return launch_rows<T, 512, 2>(a, whole, s);
+  if (vectors <= 512 * MOST) return launch_rows<T, 512, MOST>(a, whole, s);
+  if (vectors <= 512 * 8) return launch_rows<T, 512, 8>(a, whole, s);
   return launch_ex(k_rmsnorm_quantize_long<T>, dim3((unsigned)(a.rows < (1 << 20) ? a.rows : 1 << 20)), dim3(512), 0, s, true, 1, a);
 }
 
