@@ -1925,7 +1925,7 @@ int q4_linear_token_scales(const void* xq, const float* x_scale, int32_t M, cons
   if (!es) return Q4_ERR_UNSUPPORTED;
   Q4_CHECK(check_mat(w, 0, 0));
   if (w->bits != 8) return Q4_ERR_BITS;
-  if (M < 0 || w->k_pad > 131040 || out_stride < w->rows) return Q4_ERR_DIM;
+  if (M < 0 || M > INT32_MAX - 1024 || w->rows > INT32_MAX - 1024 || w->k_pad > 131040 || out_stride < w->rows) return Q4_ERR_DIM;
   if (M > 0 && (!xq || !x_scale || !out)) return Q4_ERR_NULL;
   if (!aligned16(xq) || !aligned_to(x_scale, 4) || !aligned_to(bias, 4) || !aligned_to(out, es) || !aligned_to(status, 4))
     return Q4_ERR_ALIGN;

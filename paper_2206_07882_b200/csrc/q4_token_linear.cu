@@ -1,6 +1,10 @@
 // Linear layer on 8-bit codes with a scale for every token and every output channel (q4_linear_token_scales).
 //
 // out[m, n] = (sum_k x[m, k] w[n, k]) (sx[m] sw[n]) + b[n], the sum in int32.
+//
+// Channels are the rows (lanes) of the accumulator in tensor memory and tokens its columns, whatever their numbers: a warp's 32
+// lanes store 32 neighbouring channels of one token, a channel's scale and bias stay in a register, and few tokens make a narrow
+// tile.  Codes are the tensor cores' operands as they are stored.
 #include <cuda_bf16.h>
 #include <string.h>
 
@@ -12,7 +16,7 @@ namespace q4 {
 namespace {
 
 constexpr int BK = 128;        // codes per row of an operand tile
-constexpr int CH = 128;        // output channels of a tile: the lanes of the accumulator
+constexpr int CH = 128;        // output channels of a CTA's tile
 constexpr uint32_t WAIT_LIMIT = 1u << 22;
 
 template <typename T> __device__ __forceinline__ T from_f32(float v);
@@ -20,23 +24,34 @@ template <> __device__ __forceinline__ float from_f32(float v) { return v; }
 template <> __device__ __forceinline__ __half from_f32(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32(float v) { return __float2bfloat16_rn(v); }
 
-__host__ __device__ constexpr int stages(int tok) { return tok <= 32 ? 8 : tok <= 64 ? 6 : tok <= 128 ? 6 : 4; }
-__host__ __device__ constexpr size_t smem_bytes(int tok) { return (size_t)stages(tok) * (CH + tok) * BK + 1024; }
+__device__ __forceinline__ void record_timeout(int32_t* status) {
+  if (status) atomicExch(status, Q4_ERR_TIMEOUT);
+}
 
-// Channels are the rows (lanes) of the accumulator and tokens its columns: a warp's 32 lanes store 32 neighbouring channels
-// of one token.
+// ---- one CTA a tile; up to 8 CTAs of a cluster share a tile's K
+// What few tokens need is operand bytes in flight, as their weights come from memory once: up to 216 KB in the CTAs of an SM.
+// The CTAs of a split exchange their int32 sums through distributed shared memory (in place of the rings, once all of them are
+// through), each finishing a part of the tokens, so a split changes no result.
+__host__ __device__ constexpr int stages(int tok) { return tok <= 16 ? 4 : tok <= 32 ? 5 : tok <= 64 ? 4 : 6; }
+__host__ __device__ constexpr int blocks_per_sm(int tok) { return tok <= 16 ? 3 : tok <= 64 ? 2 : 1; }
+__host__ __device__ constexpr size_t ring_bytes(int tok) { return (size_t)stages(tok) * (CH + tok) * BK; }
 template <int TOK, typename T>
-__global__ void __launch_bounds__(192, 1)
-k_token_linear(const __grid_constant__ CUtensorMap tma_w, const __grid_constant__ CUtensorMap tma_x, const TokenLinearArgs a) {
+__global__ void __launch_bounds__(192, blocks_per_sm(TOK))
+k_token_linear(const __grid_constant__ CUtensorMap tma_w, const __grid_constant__ CUtensorMap tma_x, const TokenLinearArgs a, const int tiles_n,
+               const int split) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  int32_t* part = reinterpret_cast<int32_t*>(smem);   // [split][TOK / split][CH], the sums of all CTAs of a split
+  static_assert(ring_bytes(TOK) >= (size_t)TOK * CH * 4, "sums in place of the ring");
   constexpr int NS = stages(TOK), W_BYTES = CH * BK, STAGE = W_BYTES + TOK * BK;
   constexpr uint32_t TCOLS = TOK < 32 ? 32 : TOK;
   __shared__ uint64_t full[NS], empty[NS], acc_full;
   __shared__ uint32_t tmem_base_s, failed;
   __shared__ float s_x[TOK];
   const int tid = threadIdx.x, warp = uniform_warp(), lane = tid & 31;
-  const int n0 = blockIdx.x * CH, m0 = blockIdx.y * TOK, nk = (a.K + BK - 1) / BK;
+  const int rank = blockIdx.x % split, tile = blockIdx.x / split;
+  const int n0 = tile % tiles_n * CH, m0 = tile / tiles_n * TOK, all = (a.K + BK - 1) / BK;
+  const int k0 = all * rank / split, nk = all * (rank + 1) / split - k0;   // (at least one chunk each)
   if (tid == 0) {
     for (int s = 0; s < NS; ++s) {
       mbar_init(&full[s], 1);
@@ -48,52 +63,113 @@ k_token_linear(const __grid_constant__ CUtensorMap tma_w, const __grid_constant_
     fence_proxy_async();
   }
   if (warp == 5) tmem_alloc(&tmem_base_s, TCOLS);
+  if (warp == 4 && lane == 0) {
+    prefetch_tmap(&tma_w);
+    prefetch_tmap(&tma_x);
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_base_s;
   pdl_wait();
+  bool ok = true;
   if (warp == 4) {
     const uint32_t on = elect_one();
-    bool ok = true;
-    for (int i = 0; i < nk && ok; ++i) {
-      const int s = i % NS;
-      ok = i < NS || mbar_wait_warp(&empty[s], (uint32_t)(i / NS - 1) & 1u, WAIT_LIMIT);
+    int s = 0;
+    uint32_t ph = 1;
+    for (int i = 0; i < nk; ++i) {
+      ok = i < NS || mbar_wait_warp(&empty[s], ph, WAIT_LIMIT);
       if (!ok) {
-        failed = 1;
         ring_landed(full, NS, i);
         break;
       }
       mbar_expect_tx(on, &full[s], STAGE);
-      tma_load_2d(on, smem + s * STAGE, &tma_w, i * BK, n0, &full[s]);
-      tma_load_2d(on, smem + s * STAGE + W_BYTES, &tma_x, i * BK, m0, &full[s]);
+      tma_load_2d(on, smem + s * STAGE, &tma_w, (k0 + i) * BK, n0, &full[s]);
+      tma_load_2d(on, smem + s * STAGE + W_BYTES, &tma_x, (k0 + i) * BK, m0, &full[s]);
+      if (++s == NS) {
+        s = 0;
+        ph ^= 1;
+      }
     }
   } else if (warp == 5) {
     const uint32_t idesc = umma_idesc_i8(CH, TOK), on = elect_one();
-    bool ok = true;
-    for (int i = 0; i < nk && ok; ++i) {
-      const int s = i % NS;
-      ok = mbar_wait_warp(&full[s], (uint32_t)(i / NS) & 1u, WAIT_LIMIT);
+    bool ready = mbar_test(&full[0], 0);
+    int s = 0;
+    uint32_t ph = 0;
+    for (int i = 0; i < nk; ++i) {
+      ok = mbar_wait_warp_tested(ready, &full[s], ph, WAIT_LIMIT);
       if (!ok) {
-        failed = 1;
         ring_landed(full, NS, nk);
         break;
       }
       tc_fence_after();
-      const uint64_t dw = umma_desc_sw128(smem_u32(smem + s * STAGE)), dx = umma_desc_sw128(smem_u32(smem + s * STAGE + W_BYTES));
+      const int st = s;
+      if (++s == NS) {
+        s = 0;
+        ph ^= 1;
+      }
+      ready = mbar_test(&full[s], ph);
+      const uint64_t dw = umma_desc_sw128(smem_u32(smem + st * STAGE)), dx = umma_desc_sw128(smem_u32(smem + st * STAGE + W_BYTES));
 #pragma unroll
       for (int kk = 0; kk < BK / 32; ++kk) umma_i8(on, tmem, dw + 2 * kk, dx + 2 * kk, idesc, (i | kk) != 0);
-      umma_commit(on, &empty[s]);
+      umma_commit(on, &empty[st]);
+    }
+    if (!ok) {   // recorded before the epilogue is released, so that it stores nothing
+      failed = 1;
+      __threadfence_block();
+      __syncwarp();
     }
     umma_commit(on, &acc_full);
   } else {
-    for (int c = tid; c < TOK; c += 128) s_x[c] = m0 + c < a.M ? a.x_scale[m0 + c] : 0.0f;
+    for (int c = tid; c < TOK; c += 128) s_x[c] = m0 + c < a.M ? __ldg(a.x_scale + m0 + c) : 0.0f;
     asm volatile("bar.sync 1, 128;" ::: "memory");
-    const int n = n0 + warp * 32 + lane;
-    const float sw = n < a.N ? a.w_scale[n] : 0.0f, b = a.bias && n < a.N ? a.bias[n] : 0.0f;
-    const bool ok = mbar_wait(&acc_full, 0, WAIT_LIMIT) && *reinterpret_cast<volatile uint32_t*>(&failed) == 0;
+    ok = mbar_wait(&acc_full, 0, WAIT_LIMIT);
+    ok = ok && *reinterpret_cast<volatile uint32_t*>(&failed) == 0;
     tc_fence_after();
-    if (!ok && a.status && lane == 0) atomicExch(a.status, Q4_ERR_TIMEOUT);
+  }
+  pdl_trigger();
+  if (!ok && lane == 0) {
+    record_timeout(a.status);
+    failed = 1;
+  }
+  const int ch = warp * 32 + lane, n = n0 + ch;
+  __syncwarp();
+  if (split > 1) {
+    cluster_arrive();
+    cluster_wait();                  // every CTA's products are done (or given up, with its copies landed): its ring may be written to
+    if (warp < 4) {
+      const int each = TOK / split;  // tokens that a CTA finishes
+      const uint32_t to = smem_u32(part) + (uint32_t)((rank * each) * CH + ch) * 4;
+      for (int c0 = 0; c0 < TOK; c0 += 8) {
+        int r[8];
+        tmem_ld(tmem + ((uint32_t)(warp * 32) << 16) + c0, r);
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          uint32_t addr;
+          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"(to + (uint32_t)((c0 + i) % each * CH) * 4), "r"((c0 + i) / each));
+          st_cluster(addr, r[i]);
+        }
+      }
+      if (!ok)                       // nobody stores anything of this tile
+        for (int p = 0; p < split; ++p) st_cluster(cluster_addr(&failed, p), 1);
+    }
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();
+    if (warp < 4 && n < a.N && *reinterpret_cast<volatile uint32_t*>(&failed) == 0) {
+      const int each = TOK / split, first = rank * each;
+      const float sw = __ldg(a.w_scale + n), b = a.bias ? __ldg(a.bias + n) : 0.0f;
+      T* out = static_cast<T*>(a.out) + n;
+      for (int c = 0; c < each; ++c) {
+        int sum = 0;
+        for (int p = 0; p < split; ++p) sum += part[(p * each + c) * CH + ch];
+        const int m = m0 + first + c;
+        if (m < a.M) out[(long long)m * a.ldo] = from_f32<T>(__fmaf_rn((float)sum, __fmul_rn(s_x[first + c], sw), b));
+      }
+    }
+  } else if (warp < 4) {
+    const float sw = n < a.N ? __ldg(a.w_scale + n) : 0.0f, b = a.bias && n < a.N ? __ldg(a.bias + n) : 0.0f;
     T* out = static_cast<T*>(a.out) + n;
     for (int c0 = 0; c0 < TOK; c0 += 16) {
       int r[16];
@@ -107,32 +183,236 @@ k_token_linear(const __grid_constant__ CUtensorMap tma_w, const __grid_constant_
       }
     }
   }
-  pdl_trigger();
   __syncwarp();
   tc_fence_before();
   __syncthreads();
   if (warp == 5) tmem_dealloc(tmem, TCOLS);
 }
 
-template <int TOK, typename T>
-cudaError_t launch_tile(const TokenLinearArgs& a, cudaStream_t s) {
-  static bool configured_on[MAX_DEVICES];
-  bool& configured = configured_on[device_slot()];
-  if (!configured) {
-    const cudaError_t e = cudaFuncSetAttribute(k_token_linear<TOK, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes(TOK));
-    if (e != cudaSuccess) return e;
-    configured = true;
+// ---- two CTAs a tile of 256 channels x 256 tokens, persistent
+// A stage is 128 channels and 128 tokens of 128 codes in each CTA, 32 KB for 2 x 128 x 256 x 128 products: half of what a CTA
+// alone would fetch for its 128 x 256 tile, whose operands come out of the L2 slower than the tensor cores take them.
+// Tensor memory holds two accumulators of 256 columns: the epilogue stores one while the next tile is summed up.
+constexpr int PT = 256, PAIR_STAGES = 6, PAIR_STAGE = (CH + PT / 2) * BK, PAIR_GROUP = 8;
+template <typename T>
+__global__ void __launch_bounds__(192, 1)
+k_token_linear_pair(const __grid_constant__ CUtensorMap tma_w, const __grid_constant__ CUtensorMap tma_x, const TokenLinearArgs a,
+                    const int tiles_n, const int tiles_m) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  constexpr int NS = PAIR_STAGES;
+  __shared__ uint64_t full[NS], empty[NS], acc_full[2], acc_empty[2];   // full and acc_empty: those of rank 0 count
+  __shared__ uint32_t tmem_base_s;
+  __shared__ float s_x[2][PT];
+  const int tid = threadIdx.x, warp = uniform_warp(), lane = tid & 31;
+  const uint32_t rank = pair_rank();
+  const int pairs = gridDim.x / 2, n_tiles = tiles_n * tiles_m, nk = (a.K + BK - 1) / BK;
+  if (tid == 0) {
+    for (int s = 0; s < NS; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&acc_full[b], 1);
+      mbar_init(&acc_empty[b], 8);   // the epilogue warps of both CTAs
+    }
+    fence_barrier_init();
+    fence_proxy_async();
   }
+  if (warp == 5) tmem_alloc_pair(&tmem_base_s, 2 * PT);
+  if (warp == 4 && lane == 0) {
+    prefetch_tmap(&tma_w);
+    prefetch_tmap(&tma_x);
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();                    // barriers and tensor memory of both CTAs are there
+  tc_fence_after();
+  const uint32_t tmem = tmem_base_s;
+  pdl_wait();
+  // Tiles in columns of 8 channel tiles, so that the pairs at work at one time share their operands' rows in the L2
+  auto place = [&](int t, int& n0, int& m0) {
+    const int group = t / (PAIR_GROUP * tiles_m), first = group * PAIR_GROUP, wide = min(PAIR_GROUP, tiles_n - first);
+    const int at = t - group * PAIR_GROUP * tiles_m;
+    n0 = (first + at % wide) * 2 * CH + (int)rank * CH;
+    m0 = at / wide * PT;
+  };
+  bool ok = true;
+  if (warp == 4) {
+    const uint32_t on = elect_one();
+    int s = 0, filled = 0;
+    uint32_t ph = 1;
+    for (int t = blockIdx.x / 2; t < n_tiles && ok; t += pairs) {
+      int n0, m0;
+      place(t, n0, m0);
+      for (int i = 0; i < nk; ++i) {
+        ok = filled < NS || mbar_wait_warp(&empty[s], ph, WAIT_LIMIT);
+        if (!ok) break;
+        ++filled;
+        const uint32_t bar = cluster_addr(&full[s], 0);
+        if (rank == 0) mbar_expect_tx(on, &full[s], 2 * PAIR_STAGE);
+        tma_load_2d_pair(on, smem + s * PAIR_STAGE, &tma_w, i * BK, n0, bar);
+        tma_load_2d_pair(on, smem + s * PAIR_STAGE + CH * BK, &tma_x, i * BK, m0 + (int)rank * (PT / 2), bar);
+        if (++s == NS) {
+          s = 0;
+          ph ^= 1;
+        }
+      }
+    }
+    if (ok) {   // the last MMAs' arrivals on this CTA's barriers are in before it can leave
+      for (int j = 0; j < min(filled, NS); ++j)
+        ok = mbar_wait_warp(&empty[j], (uint32_t)((filled - j + NS - 1) / NS - 1) & 1u, WAIT_LIMIT) && ok;
+    } else if (rank == 0) {
+      ring_landed(full, NS, filled);
+    }
+  } else if (warp == 5) {
+    if (rank == 0) {
+      const uint32_t idesc = umma_idesc_i8(2 * CH, PT), on = elect_one();
+      bool ready = mbar_test(&full[0], 0);
+      int s = 0, it = 0, used = 0;
+      uint32_t ph = 0;
+      for (int t = blockIdx.x / 2; t < n_tiles && ok; t += pairs, ++it) {
+        const int buf = it & 1, use = it >> 1;
+        if (use >= 1) ok = __all_sync(0xffffffffu, mbar_wait_cluster(&acc_empty[buf], (use - 1) & 1, WAIT_LIMIT)) != 0;
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t d = tmem + (uint32_t)(buf * PT);
+        for (int i = 0; i < nk; ++i) {
+          ok = mbar_wait_warp_tested(ready, &full[s], ph, WAIT_LIMIT);
+          if (!ok) break;
+          ++used;
+          tc_fence_after();
+          const int st = s;
+          if (++s == NS) {
+            s = 0;
+            ph ^= 1;
+          }
+          ready = mbar_test(&full[s], ph);
+          const uint64_t dw = umma_desc_sw128(smem_u32(smem + st * PAIR_STAGE)), dx = umma_desc_sw128(smem_u32(smem + st * PAIR_STAGE + CH * BK));
+#pragma unroll
+          for (int kk = 0; kk < BK / 32; ++kk) umma_i8_pair(on, d, dw + 2 * kk, dx + 2 * kk, idesc, (i | kk) != 0);
+          umma_commit_pair(on, &empty[st]);
+        }
+        if (ok) umma_commit_pair(on, &acc_full[buf]);
+      }
+      if (!ok) ring_landed(full, NS, used + NS);   // what the producers may have issued
+    }
+  } else {
+    int it = 0;
+    for (int t = blockIdx.x / 2; t < n_tiles; t += pairs, ++it) {
+      const int buf = it & 1, use = it >> 1;
+      int n0, m0;
+      place(t, n0, m0);
+      const int n = n0 + warp * 32 + lane;
+      for (int c = tid; c < PT; c += 128) s_x[buf][c] = m0 + c < a.M ? __ldg(a.x_scale + m0 + c) : 0.0f;
+      const float sw = n < a.N ? __ldg(a.w_scale + n) : 0.0f, b = a.bias && n < a.N ? __ldg(a.bias + n) : 0.0f;
+      asm volatile("bar.sync 1, 128;" ::: "memory");   // (nobody is still at the tile before the last, which used this buffer)
+      ok = ok && __all_sync(0xffffffffu, mbar_wait_cluster(&acc_full[buf], use & 1, WAIT_LIMIT)) != 0;
+      if (!ok) continue;                               // stores nothing any more, but meets the others at the barrier
+      tc_fence_after();
+      const uint32_t taddr = tmem + (uint32_t)(buf * PT) + ((uint32_t)(warp * 32) << 16);
+      T* out = static_cast<T*>(a.out) + n + (long long)m0 * a.ldo;
+      const int tokens = n < a.N ? min(PT, a.M - m0) : 0;
+      int r0[32], r1[32];
+      auto store32 = [&](const int (&r)[32], int c0) {
+        if (c0 + 32 <= tokens) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            *out = from_f32<T>(__fmaf_rn((float)r[i], __fmul_rn(s_x[buf][c0 + i], sw), b));
+            out += a.ldo;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            if (c0 + i < tokens) *out = from_f32<T>(__fmaf_rn((float)r[i], __fmul_rn(s_x[buf][c0 + i], sw), b));
+            out += a.ldo;
+          }
+        }
+      };
+      tmem_ld32(taddr, r0);
+#pragma unroll 1
+      for (int c0 = 0; c0 < PT; c0 += 64) {
+        tmem_ld_wait();
+        tmem_ld32(taddr + c0 + 32, r1);
+        store32(r0, c0);
+        tmem_ld_wait();
+        if (c0 + 64 < PT) {
+          tmem_ld32(taddr + c0 + 64, r0);
+        } else {   // the accumulator has been read: hand it back before the last stores
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(cluster_addr(&acc_empty[buf], 0));
+        }
+        store32(r1, c0 + 32);
+      }
+    }
+  }
+  pdl_trigger();
+  if (!ok && lane == 0) record_timeout(a.status);
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();                    // no CTA leaves, or frees its tensor memory, while the other may still use it
+  if (warp == 5) tmem_dealloc_pair(tmem, 2 * PT);
+}
+
+template <typename K>
+cudaError_t allow_smem(K kernel, size_t bytes, bool* configured_on) {
+  bool& configured = configured_on[device_slot()];
+  if (configured) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  configured = e == cudaSuccess;
+  return e;
+}
+
+template <int TOK, typename T>
+cudaError_t launch_tile(const TokenLinearArgs& a, int split, cudaStream_t s) {
+  static bool configured_on[MAX_DEVICES];
+  const size_t bytes = ring_bytes(TOK) + 1024;
+  cudaError_t e = allow_smem(k_token_linear<TOK, T>, bytes, configured_on);
+  if (e != cudaSuccess) return e;
   CUtensorMap tw, tx;
   if (!make_tmap_i8(&tw, a.wq, a.K, a.N, a.K, CH) || !make_tmap_i8(&tx, a.xq, a.K, a.M, a.K, TOK)) return cudaErrorInvalidValue;
-  return launch_ex(k_token_linear<TOK, T>, dim3((a.N + CH - 1) / CH, (a.M + TOK - 1) / TOK), dim3(192), smem_bytes(TOK), s, true, 1,
-                   tw, tx, a);
+  const int tiles_n = (a.N + CH - 1) / CH, tiles_m = (a.M + TOK - 1) / TOK;
+  return launch_ex(k_token_linear<TOK, T>, dim3((unsigned)(tiles_n * tiles_m * split)), dim3(192), bytes, s, true, (unsigned)split, tw, tx, a,
+                   tiles_n, split);
 }
 template <typename T>
+cudaError_t launch_pair(const TokenLinearArgs& a, cudaStream_t s) {
+  static bool configured_on[MAX_DEVICES];
+  const size_t bytes = (size_t)PAIR_STAGES * PAIR_STAGE + 1024;
+  cudaError_t e = allow_smem(k_token_linear_pair<T>, bytes, configured_on);
+  if (e != cudaSuccess) return e;
+  CUtensorMap tw, tx;
+  if (!make_tmap_i8(&tw, a.wq, a.K, a.N, a.K, CH) || !make_tmap_i8(&tx, a.xq, a.K, a.M, a.K, PT / 2)) return cudaErrorInvalidValue;
+  const int tiles_n = (a.N + 2 * CH - 1) / (2 * CH), tiles_m = (a.M + PT - 1) / PT;
+  const long long tiles = (long long)tiles_n * tiles_m;
+  if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
+  const int pairs = tiles < sm_count() / 2 ? (int)tiles : sm_count() / 2;
+  return launch_ex(k_token_linear_pair<T>, dim3((unsigned)(2 * pairs)), dim3(192), bytes, s, true, 2, tw, tx, a, tiles_n, tiles_m);
+}
+
+template <typename T>
 cudaError_t launch_typed(const TokenLinearArgs& a, cudaStream_t s) {
-  return a.M <= 16   ? launch_tile<16, T>(a, s)
-         : a.M <= 64 ? launch_tile<64, T>(a, s)
-                     : launch_tile<256, T>(a, s);
+  const long long sms = sm_count(), tiles_n = (a.N + CH - 1) / CH, chunks = (a.K + BK - 1) / BK;
+  // Pairs of CTAs once their tiles fill three quarters of the device
+  const long long pair_tiles = (long long)((a.N + 2 * CH - 1) / (2 * CH)) * ((a.M + PT - 1) / PT);
+  if (a.M > 64 && pair_tiles * 8 >= sms * 3) return launch_pair<T>(a, s);
+  // One tile for all of few tokens, else the widest that still gives every SM one
+  int tok = a.M <= 16 ? 16 : a.M <= 32 ? 32 : a.M <= 64 ? 64 : 128;
+  if (a.M > 64)
+    while (tok > 32 && tiles_n * ((a.M + tok - 1) / tok) < sms) tok /= 2;
+  // and a split of K while there are fewer tiles than SMs, two chunks at least for each part
+  int split = 1;
+  const long long tiles = tiles_n * ((a.M + tok - 1) / tok);
+  while (split < 8 && tiles * split < sms && chunks >= 4 * split) split *= 2;
+  if (tiles * split > INT32_MAX / 2) return cudaErrorInvalidValue;
+  return tok == 16    ? launch_tile<16, T>(a, split, s)
+         : tok == 32  ? launch_tile<32, T>(a, split, s)
+         : tok == 64  ? launch_tile<64, T>(a, split, s)
+                      : launch_tile<128, T>(a, split, s);
 }
 
 }  // namespace
