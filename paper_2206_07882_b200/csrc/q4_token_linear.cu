@@ -6,6 +6,7 @@
 // lanes store 32 neighbouring channels of one token, a channel's scale and bias stay in a register, and few tokens make a narrow
 // tile.  Codes are the tensor cores' operands as they are stored.
 #include <cuda_bf16.h>
+#include <math.h>
 #include <string.h>
 
 #include "q4_internal.h"
@@ -28,24 +29,56 @@ __device__ __forceinline__ void record_timeout(int32_t* status) {
   if (status) atomicExch(status, Q4_ERR_TIMEOUT);
 }
 
+// COLS accumulator columns of a warp's 32 lanes, from `taddr` on, to tokens 0 .. min(COLS, tokens) - 1 at `out` (this lane's channel).
+// Two sets of registers: the next columns are on their way out of tensor memory while these are stored; `drained` is called once
+// all have been read.
+template <typename T, int COLS, typename F>
+__device__ __forceinline__ void store_columns(uint32_t taddr, T* out, long long ldo, const float* scale, float sw, float b, int tokens, F drained) {
+  constexpr int STEP = COLS < 32 ? COLS : 32;
+  int r[2][STEP];
+  tmem_ld(taddr, r[0]);
+#pragma unroll
+  for (int c0 = 0; c0 < COLS; c0 += STEP) {
+    const int set = c0 / STEP & 1;
+    tmem_ld_wait();
+    if (c0 + STEP < COLS)
+      tmem_ld(taddr + c0 + STEP, r[set ^ 1]);
+    else
+      drained();
+    if (c0 + STEP <= tokens) {
+#pragma unroll
+      for (int i = 0; i < STEP; ++i) {
+        *out = from_f32<T>(__fmaf_rn((float)r[set][i], __fmul_rn(scale[c0 + i], sw), b));
+        out += ldo;
+      }
+    } else if (c0 < tokens) {
+#pragma unroll
+      for (int i = 0; i < STEP; ++i) {
+        if (c0 + i < tokens) *out = from_f32<T>(__fmaf_rn((float)r[set][i], __fmul_rn(scale[c0 + i], sw), b));
+        out += ldo;
+      }
+    }
+  }
+}
+
 // ---- one CTA a tile; up to 8 CTAs of a cluster share a tile's K
 // What few tokens need is operand bytes in flight, as their weights come from memory once: up to 216 KB in the CTAs of an SM.
 // The CTAs of a split exchange their int32 sums through distributed shared memory (in place of the rings, once all of them are
 // through), each finishing a part of the tokens, so a split changes no result.
-__host__ __device__ constexpr int stages(int tok) { return tok <= 16 ? 4 : tok <= 32 ? 5 : tok <= 64 ? 4 : 6; }
+constexpr int MAX_STAGES = 12;
+constexpr size_t RING_SM = 216 * 1024;   // bytes of rings on an SM
+__host__ __device__ constexpr int stage_bytes(int tok) { return (CH + tok) * BK; }
 __host__ __device__ constexpr int blocks_per_sm(int tok) { return tok <= 16 ? 3 : tok <= 64 ? 2 : 1; }
-__host__ __device__ constexpr size_t ring_bytes(int tok) { return (size_t)stages(tok) * (CH + tok) * BK; }
 template <int TOK, typename T>
 __global__ void __launch_bounds__(192, blocks_per_sm(TOK))
 k_token_linear(const __grid_constant__ CUtensorMap tma_w, const __grid_constant__ CUtensorMap tma_x, const TokenLinearArgs a, const int tiles_n,
-               const int split) {
+               const int split, const int NS) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   int32_t* part = reinterpret_cast<int32_t*>(smem);   // [split][TOK / split][CH], the sums of all CTAs of a split
-  static_assert(ring_bytes(TOK) >= (size_t)TOK * CH * 4, "sums in place of the ring");
-  constexpr int NS = stages(TOK), W_BYTES = CH * BK, STAGE = W_BYTES + TOK * BK;
+  constexpr int W_BYTES = CH * BK, STAGE = W_BYTES + TOK * BK;
   constexpr uint32_t TCOLS = TOK < 32 ? 32 : TOK;
-  __shared__ uint64_t full[NS], empty[NS], acc_full;
+  __shared__ uint64_t full[MAX_STAGES], empty[MAX_STAGES], acc_full;
   __shared__ uint32_t tmem_base_s, failed;
   __shared__ float s_x[TOK];
   const int tid = threadIdx.x, warp = uniform_warp(), lane = tid & 31;
@@ -135,6 +168,7 @@ k_token_linear(const __grid_constant__ CUtensorMap tma_w, const __grid_constant_
   const int ch = warp * 32 + lane, n = n0 + ch;
   __syncwarp();
   if (split > 1) {
+    const int log_each = 31 - __clz(TOK / split);
     cluster_arrive();
     cluster_wait();                  // every CTA's products are done (or given up, with its copies landed): its ring may be written to
     if (warp < 4) {
@@ -145,10 +179,12 @@ k_token_linear(const __grid_constant__ CUtensorMap tma_w, const __grid_constant_
         tmem_ld(tmem + ((uint32_t)(warp * 32) << 16) + c0, r);
         tmem_ld_wait();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 8; i += 2) {   // (each is 2 at least)
+          const int dst = (c0 + i) >> log_each;
           uint32_t addr;
-          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"(to + (uint32_t)((c0 + i) % each * CH) * 4), "r"((c0 + i) / each));
+          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"(to + (uint32_t)(((c0 + i) & (each - 1)) * CH) * 4), "r"(dst));
           st_cluster(addr, r[i]);
+          st_cluster(addr + CH * 4, r[i + 1]);
         }
       }
       if (!ok)                       // nobody stores anything of this tile
@@ -170,18 +206,8 @@ k_token_linear(const __grid_constant__ CUtensorMap tma_w, const __grid_constant_
     }
   } else if (warp < 4) {
     const float sw = n < a.N ? __ldg(a.w_scale + n) : 0.0f, b = a.bias && n < a.N ? __ldg(a.bias + n) : 0.0f;
-    T* out = static_cast<T*>(a.out) + n;
-    for (int c0 = 0; c0 < TOK; c0 += 16) {
-      int r[16];
-      tmem_ld16(tmem + ((uint32_t)(warp * 32) << 16) + c0, r);
-      tmem_ld_wait();
-      if (!ok || n >= a.N) continue;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int m = m0 + c0 + i;
-        if (m < a.M) out[(long long)m * a.ldo] = from_f32<T>(__fmaf_rn((float)r[i], __fmul_rn(s_x[c0 + i], sw), b));
-      }
-    }
+    store_columns<T, TOK>(tmem + ((uint32_t)(warp * 32) << 16), static_cast<T*>(a.out) + (long long)m0 * a.ldo + n, a.ldo, s_x, sw, b,
+                          ok && n < a.N ? a.M - m0 : 0, [] {});
   }
   __syncwarp();
   tc_fence_before();
@@ -195,7 +221,7 @@ k_token_linear(const __grid_constant__ CUtensorMap tma_w, const __grid_constant_
 // Tensor memory holds two accumulators of 256 columns: the epilogue stores one while the next tile is summed up.
 constexpr int PT = 256, PAIR_STAGES = 6, PAIR_STAGE = (CH + PT / 2) * BK, PAIR_GROUP = 8;
 template <typename T>
-__global__ void __launch_bounds__(192, 1)
+__global__ void __launch_bounds__(320, 1)
 k_token_linear_pair(const __grid_constant__ CUtensorMap tma_w, const __grid_constant__ CUtensorMap tma_x, const TokenLinearArgs a,
                     const int tiles_n, const int tiles_m) {
   extern __shared__ uint8_t smem_raw[];
@@ -214,13 +240,13 @@ k_token_linear_pair(const __grid_constant__ CUtensorMap tma_w, const __grid_cons
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(&acc_full[b], 1);
-      mbar_init(&acc_empty[b], 8);   // the epilogue warps of both CTAs
+      mbar_init(&acc_empty[b], 16);   // the epilogue warps of both CTAs
     }
     fence_barrier_init();
     fence_proxy_async();
   }
-  if (warp == 5) tmem_alloc_pair(&tmem_base_s, 2 * PT);
-  if (warp == 4 && lane == 0) {
+  if (warp == 9) tmem_alloc_pair(&tmem_base_s, 2 * PT);
+  if (warp == 8 && lane == 0) {
     prefetch_tmap(&tma_w);
     prefetch_tmap(&tma_x);
   }
@@ -239,7 +265,7 @@ k_token_linear_pair(const __grid_constant__ CUtensorMap tma_w, const __grid_cons
     m0 = at / wide * PT;
   };
   bool ok = true;
-  if (warp == 4) {
+  if (warp == 8) {
     const uint32_t on = elect_one();
     int s = 0, filled = 0;
     uint32_t ph = 1;
@@ -266,7 +292,7 @@ k_token_linear_pair(const __grid_constant__ CUtensorMap tma_w, const __grid_cons
     } else if (rank == 0) {
       ring_landed(full, NS, filled);
     }
-  } else if (warp == 5) {
+  } else if (warp == 9) {
     if (rank == 0) {
       const uint32_t idesc = umma_idesc_i8(2 * CH, PT), on = elect_one();
       bool ready = mbar_test(&full[0], 0);
@@ -304,48 +330,20 @@ k_token_linear_pair(const __grid_constant__ CUtensorMap tma_w, const __grid_cons
       const int buf = it & 1, use = it >> 1;
       int n0, m0;
       place(t, n0, m0);
-      const int n = n0 + warp * 32 + lane;
-      for (int c = tid; c < PT; c += 128) s_x[buf][c] = m0 + c < a.M ? __ldg(a.x_scale + m0 + c) : 0.0f;
+      const int n = n0 + warp % 4 * 32 + lane, first = warp / 4 * (PT / 2);   // four warps for each half of the tokens
+      for (int c = tid; c < PT; c += 256) s_x[buf][c] = m0 + c < a.M ? __ldg(a.x_scale + m0 + c) : 0.0f;
       const float sw = n < a.N ? __ldg(a.w_scale + n) : 0.0f, b = a.bias && n < a.N ? __ldg(a.bias + n) : 0.0f;
-      asm volatile("bar.sync 1, 128;" ::: "memory");   // (nobody is still at the tile before the last, which used this buffer)
+      asm volatile("bar.sync 1, 256;" ::: "memory");   // (nobody is still at the tile before the last, which used this buffer)
       ok = ok && __all_sync(0xffffffffu, mbar_wait_cluster(&acc_full[buf], use & 1, WAIT_LIMIT)) != 0;
       if (!ok) continue;                               // stores nothing any more, but meets the others at the barrier
       tc_fence_after();
-      const uint32_t taddr = tmem + (uint32_t)(buf * PT) + ((uint32_t)(warp * 32) << 16);
-      T* out = static_cast<T*>(a.out) + n + (long long)m0 * a.ldo;
-      const int tokens = n < a.N ? min(PT, a.M - m0) : 0;
-      int r0[32], r1[32];
-      auto store32 = [&](const int (&r)[32], int c0) {
-        if (c0 + 32 <= tokens) {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            *out = from_f32<T>(__fmaf_rn((float)r[i], __fmul_rn(s_x[buf][c0 + i], sw), b));
-            out += a.ldo;
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            if (c0 + i < tokens) *out = from_f32<T>(__fmaf_rn((float)r[i], __fmul_rn(s_x[buf][c0 + i], sw), b));
-            out += a.ldo;
-          }
-        }
-      };
-      tmem_ld32(taddr, r0);
-#pragma unroll 1
-      for (int c0 = 0; c0 < PT; c0 += 64) {
-        tmem_ld_wait();
-        tmem_ld32(taddr + c0 + 32, r1);
-        store32(r0, c0);
-        tmem_ld_wait();
-        if (c0 + 64 < PT) {
-          tmem_ld32(taddr + c0 + 64, r0);
-        } else {   // the accumulator has been read: hand it back before the last stores
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(cluster_addr(&acc_empty[buf], 0));
-        }
-        store32(r1, c0 + 32);
-      }
+      const uint32_t taddr = tmem + (uint32_t)(buf * PT + first) + ((uint32_t)(warp % 4 * 32) << 16);
+      store_columns<T, PT / 2>(taddr, static_cast<T*>(a.out) + n + (long long)(m0 + first) * a.ldo, a.ldo, s_x[buf] + first, sw, b,
+                               n < a.N ? a.M - m0 - first : 0, [&] {   // hand the accumulator back before the last stores
+                                 tc_fence_before();
+                                 __syncwarp();
+                                 if (lane == 0) mbar_arrive_cluster(cluster_addr(&acc_empty[buf], 0));
+                               });
     }
   }
   pdl_trigger();
@@ -355,7 +353,7 @@ k_token_linear_pair(const __grid_constant__ CUtensorMap tma_w, const __grid_cons
   __syncthreads();
   cluster_arrive();
   cluster_wait();                    // no CTA leaves, or frees its tensor memory, while the other may still use it
-  if (warp == 5) tmem_dealloc_pair(tmem, 2 * PT);
+  if (warp == 9) tmem_dealloc_pair(tmem, 2 * PT);
 }
 
 template <typename K>
@@ -370,14 +368,19 @@ cudaError_t allow_smem(K kernel, size_t bytes, bool* configured_on) {
 template <int TOK, typename T>
 cudaError_t launch_tile(const TokenLinearArgs& a, int split, cudaStream_t s) {
   static bool configured_on[MAX_DEVICES];
-  const size_t bytes = ring_bytes(TOK) + 1024;
-  cudaError_t e = allow_smem(k_token_linear<TOK, T>, bytes, configured_on);
+  cudaError_t e = allow_smem(k_token_linear<TOK, T>, RING_SM + 1024, configured_on);
   if (e != cudaSuccess) return e;
   CUtensorMap tw, tx;
   if (!make_tmap_i8(&tw, a.wq, a.K, a.N, a.K, CH) || !make_tmap_i8(&tx, a.xq, a.K, a.M, a.K, TOK)) return cudaErrorInvalidValue;
   const int tiles_n = (a.N + CH - 1) / CH, tiles_m = (a.M + TOK - 1) / TOK;
-  return launch_ex(k_token_linear<TOK, T>, dim3((unsigned)(tiles_n * tiles_m * split)), dim3(192), bytes, s, true, (unsigned)split, tw, tx, a,
-                   tiles_n, split);
+  // the CTAs of an SM share the room for rings; a ring needs no more stages than its part of K has chunks, but holds the sums of a split
+  const long long ctas = (long long)tiles_n * tiles_m * split, each = (ctas + sm_count() - 1) / sm_count();
+  const int on_sm = each < blocks_per_sm(TOK) ? (int)each : blocks_per_sm(TOK), chunks = ((a.K + BK - 1) / BK + split - 1) / split;
+  int ns = (int)((RING_SM - 1024 * on_sm) / on_sm / stage_bytes(TOK));
+  ns = ns < chunks ? ns : chunks;
+  ns = ns < 4 ? 4 : ns > MAX_STAGES ? MAX_STAGES : ns;
+  const size_t bytes = (size_t)ns * stage_bytes(TOK) + 1024;
+  return launch_ex(k_token_linear<TOK, T>, dim3((unsigned)ctas), dim3(192), bytes, s, true, (unsigned)split, tw, tx, a, tiles_n, split, ns);
 }
 template <typename T>
 cudaError_t launch_pair(const TokenLinearArgs& a, cudaStream_t s) {
@@ -391,28 +394,56 @@ cudaError_t launch_pair(const TokenLinearArgs& a, cudaStream_t s) {
   const long long tiles = (long long)tiles_n * tiles_m;
   if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
   const int pairs = tiles < sm_count() / 2 ? (int)tiles : sm_count() / 2;
-  return launch_ex(k_token_linear_pair<T>, dim3((unsigned)(2 * pairs)), dim3(192), bytes, s, true, 2, tw, tx, a, tiles_n, tiles_m);
+  return launch_ex(k_token_linear_pair<T>, dim3((unsigned)(2 * pairs)), dim3(320), bytes, s, true, 2, tw, tx, a, tiles_n, tiles_m);
+}
+
+// Time of a launch in us, fitted to all kernels' times at some 35 shapes (1 to 8192 tokens, 100 to 32000 channels, 100 to 8192 codes);
+// the kernel with the least is taken.  At those shapes the choice is the fastest or within a fifth of it.  Examples, us for 32 /
+// 64 / 128 tokens a tile / pairs: 128 x 4096 x 4096 7.6 / 8.5 / 10.5 / 14.1, 1024 x 4096 x 4096 38 / 24 / 21 / 15.6.
+// A CTA alone: a tile's chunk of 128 codes takes as long as its operands need from the L2 (18 to 32 KB), the CTAs of an SM one after
+// the other, their epilogues behind the first, and all bytes at least their time in memory.  A split costs 1.6 us more and pays
+// where few tiles have a long K (16 x 1024 x 4096: 5.6 -> 3.8); with more CTAs than SMs it never did.
+double memory_time(const TokenLinearArgs& a, int bytes) { return ((double)a.N * a.K + (double)a.M * a.K + (double)a.M * a.N * bytes) / 6.2e6; }
+double single_cost(const TokenLinearArgs& a, int tok, int split, int bytes) {
+  const double chunk = tok == 16 ? 0.13 : tok == 32 ? 0.155 : tok == 64 ? 0.19 : 0.27;
+  const int chunks = ((a.K + BK - 1) / BK + split - 1) / split;
+  const double each = ceil((double)((a.N + CH - 1) / CH) * ((a.M + tok - 1) / tok) * split / sm_count());
+  const double memory = memory_time(a, bytes), sums = each * chunks * chunk + (each - 1.0) * 0.025 * tok;
+  return 2.6 + (split > 1 ? 1.6 : 0.0) + (memory > sums ? memory : sums);
+}
+// A pair: 0.33 us a chunk for both its CTAs' 256 x 256; rounds of tiles behind the first at least their epilogue.
+double pair_cost(const TokenLinearArgs& a, int bytes) {
+  const long long tiles = (long long)((a.N + 2 * CH - 1) / (2 * CH)) * ((a.M + PT - 1) / PT), pairs = sm_count() / 2;
+  const double chunks = 0.33 * ((a.K + BK - 1) / BK), memory = memory_time(a, bytes);
+  const double sums = chunks + (double)((tiles + pairs - 1) / pairs - 1) * (chunks > 3.0 ? chunks : 3.0);
+  return 6.0 + (memory > sums ? memory : sums);
 }
 
 template <typename T>
 cudaError_t launch_typed(const TokenLinearArgs& a, cudaStream_t s) {
-  const long long sms = sm_count(), tiles_n = (a.N + CH - 1) / CH, chunks = (a.K + BK - 1) / BK;
-  // Pairs of CTAs once their tiles fill three quarters of the device
-  const long long pair_tiles = (long long)((a.N + 2 * CH - 1) / (2 * CH)) * ((a.M + PT - 1) / PT);
-  if (a.M > 64 && pair_tiles * 8 >= sms * 3) return launch_pair<T>(a, s);
-  // One tile for all of few tokens, else the widest that still gives every SM one
-  int tok = a.M <= 16 ? 16 : a.M <= 32 ? 32 : a.M <= 64 ? 64 : 128;
-  if (a.M > 64)
-    while (tok > 32 && tiles_n * ((a.M + tok - 1) / tok) < sms) tok /= 2;
-  // and a split of K while there are fewer tiles than SMs, two chunks at least for each part
-  int split = 1;
-  const long long tiles = tiles_n * ((a.M + tok - 1) / tok);
-  while (split < 8 && tiles * split < sms && chunks >= 4 * split) split *= 2;
-  if (tiles * split > INT32_MAX / 2) return cudaErrorInvalidValue;
-  return tok == 16    ? launch_tile<16, T>(a, split, s)
-         : tok == 32  ? launch_tile<32, T>(a, split, s)
-         : tok == 64  ? launch_tile<64, T>(a, split, s)
-                      : launch_tile<128, T>(a, split, s);
+  const int chunks = (a.K + BK - 1) / BK;
+  double least = a.M > 64 ? pair_cost(a, sizeof(T)) : 1e300;
+  int tok = 0, split = 1;
+  for (int t = 16; t <= 128; t *= 2) {
+    if (t == 16 ? a.M > 16 : t / 2 >= a.M) continue;                  // (more tiles of 16 tokens never paid)
+    const long long tiles = (long long)((a.N + CH - 1) / CH) * ((a.M + t - 1) / t);
+    for (int p = 1; p <= (t <= 32 ? 8 : 1); p *= p == 1 ? 4 : 2) {   // two chunks at least for each part
+      if (p > 1 && (chunks < 2 * p || tiles * p > sm_count())) break;
+      const double c = single_cost(a, t, p, sizeof(T));
+      if (c < least) {
+        least = c;
+        tok = t;
+        split = p;
+      }
+    }
+  }
+  if (tok == 0) return launch_pair<T>(a, s);
+  const long long ctas = (long long)((a.N + CH - 1) / CH) * ((a.M + tok - 1) / tok) * split;
+  if (ctas > INT32_MAX / 2) return cudaErrorInvalidValue;
+  return tok == 16   ? launch_tile<16, T>(a, split, s)
+         : tok == 32 ? launch_tile<32, T>(a, split, s)
+         : tok == 64 ? launch_tile<64, T>(a, split, s)
+                     : launch_tile<128, T>(a, split, s);
 }
 
 }  // namespace

@@ -176,6 +176,13 @@ def test_linear(Bd, M, N, K, dtype):
     check_linear(Bd, x, w, sx, sw, b, dtype, gap=(M + K) % 3, k=K)
 
 
+@pytest.mark.parametrize("M,N,K", [(2048, 2050, 160), (70, 14500, 64), (1800, 2000, 1283), (600, 5000, 31), (9000, 640, 260), (257, 40000, 96)])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_linear_of_many_tiles(Bd, M, N, K, dtype):
+    x, w, sx, sw, b = linear_inputs(M, N, K, M + N + K, bias=N % 4 == 0)
+    check_linear(Bd, x, w, sx, sw, b, dtype, gap=M % 3, k=K)
+
+
 @pytest.mark.parametrize("M", [2, 70, 300])
 def test_linear_of_the_longest_rows(Bd, M):
     # every product 2^14: the sum of 131040 of them is just below 2^31
