@@ -86,6 +86,8 @@ class ReorderS(C.Structure):
                 ("dst_step", C.c_int64 * 2)]
 
 
+_REORDER_ARRAYS = [ReorderS * n for n in range(REORDER_MAX + 1)]     # (making an array type takes longer than filling it)
+
 EXPORTS = ["q4_act_symmetric", "q4_act_asymmetric", "quantize_pack_int4", "qlstm_layer_forward",
            "qlstm_step", "q4_linear_forward", "qjoint_logprobs", "q4_beam_init",
            "dr_fusion_beam_step", "q4_beam_search", "q4_search_plan_create", "q4_search_plan_destroy", "q4_search_plan_info", "q4_search_steps_taken", "q4_traceback", "q4_feature_prologue", "q4_workspace_bytes",
@@ -701,11 +703,11 @@ def q4_beam_reorder(pairs: Sequence, parent: torch.Tensor, dim: int = 0):
     if dim < 0:
         raise ValueError("dim: not negative")
     B, W = parent.shape
+    dev = _on_device(parent, *(t for pair in pairs for t in pair))
     for first in range(0, len(pairs), REORDER_MAX):
         group = pairs[first:first + REORDER_MAX]
-        items = (ReorderS * len(group))()
+        items = _REORDER_ARRAYS[len(group)]()
         for item, (src, dst) in zip(items, group):
-            dev = _on_device(parent, src, dst)
             _reorder_item(item, src, dst, dim, B, W)
         _chk(lib().q4_beam_reorder(items, len(group), parent.data_ptr(), B, W, torch._C._cuda_getCurrentRawStream(dev)),
              "q4_beam_reorder")

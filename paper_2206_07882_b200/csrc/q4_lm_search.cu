@@ -547,13 +547,19 @@ __global__ void __launch_bounds__(ROW_NT, ROW_BLOCKS) k_lm_select(const LmSelect
   if (last_to_arrive(a.arrived + utterance, a.W, sh)) merge_rows(a, p, utterance, sh);
 }
 
-// Moves of up to Q4_REORDER_MAX tensors, cut into vectors of `width` bytes.
+// Moves of up to Q4_REORDER_MAX tensors, rows cut into vectors of `width` bytes.  A block takes a piece of one long row or some
+// short rows; where its rows lie is worked out once a row and kept in shared memory, so that a vector costs one 32-bit multiplication
+// beside its load and store.
 struct MoveItem {
   const uint8_t* src;
   uint8_t* dst;
   long long src_row, dst_row, src_step[2], dst_step[2];
-  long long n0, n1, per_row;   // vectors of a row
+  long long rows, n1, per_row;    // rows of all steps; vectors of a row
+  long long piece;                // vectors of a row that a block takes
   int32_t width;
+  int32_t block_rows;             // rows of a block; more than one: whole rows
+  uint32_t pieces;                // blocks of a row
+  uint32_t over;                  // 2^32 / per_row, rounded up, for blocks of several rows
   uint32_t first_block;
 };
 struct Moves {
@@ -561,35 +567,59 @@ struct Moves {
   int32_t n_items, B, W;
   const int32_t* parent;
 };
-constexpr int MOVE_VECTORS = 1024;   // of a block
+constexpr int MOVE_NT = 256, MOVE_EACH = 8, MOVE_ROWS = 256;   // vectors of a thread, most rows of a block
+constexpr int MOVE_VECTORS = MOVE_NT * MOVE_EACH;
 
 template <typename V>
-__device__ __forceinline__ void move_vectors(const MoveItem& t, const Moves& a, long long base) {
-  const long long total = t.n0 * t.n1 * a.B * a.W * t.per_row;
-  for (int i = threadIdx.x; i < MOVE_VECTORS; i += blockDim.x) {
-    const long long v = base + i;
-    if (v >= total) return;
-    const long long r = v / t.per_row, col = v % t.per_row;
-    const long long i1 = r % t.n1, bw = (r / t.n1) % ((long long)a.B * a.W), i0 = r / t.n1 / ((long long)a.B * a.W);
-    const int p = a.parent[bw];
-    if (p < 0 || p >= a.W) continue;
-    const long long from = bw / a.W * a.W + p;
-    reinterpret_cast<V*>(t.dst + i0 * t.dst_step[0] + i1 * t.dst_step[1] + bw * t.dst_row)[col] =
-        reinterpret_cast<const V*>(t.src + i0 * t.src_step[0] + i1 * t.src_step[1] + from * t.src_row)[col];
+__device__ __forceinline__ void move_vectors(const MoveItem& t, const uint8_t* const* from, uint8_t* const* to, long long first, int n) {
+#pragma unroll 1
+  for (int i0 = threadIdx.x; i0 < n; i0 += MOVE_NT * 4) {
+    V v[4];
+    V* at[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {   // loads of four vectors, then their stores
+      const int i = i0 + j * MOVE_NT;
+      at[j] = nullptr;
+      if (i >= n) continue;
+      const int r = t.block_rows == 1 ? 0 : t.per_row == 1 ? i : (int)__umulhi((uint32_t)i, t.over);
+      const long long col = t.block_rows > 1 ? i - r * (int)t.per_row : first + i;
+      if (to[r] == nullptr) continue;
+      v[j] = __ldg(reinterpret_cast<const V*>(from[r]) + col);
+      at[j] = reinterpret_cast<V*>(to[r]) + col;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (at[j]) *at[j] = v[j];
   }
 }
 
-__global__ void __launch_bounds__(256) k_beam_reorder(const __grid_constant__ Moves a) {
+__global__ void __launch_bounds__(MOVE_NT) k_beam_reorder(const __grid_constant__ Moves a) {
+  __shared__ const uint8_t* s_from[MOVE_ROWS];
+  __shared__ uint8_t* s_to[MOVE_ROWS];     // null: left as it is
   int it = 0;
   while (it + 1 < a.n_items && blockIdx.x >= a.item[it + 1].first_block) ++it;
   const MoveItem& t = a.item[it];
-  const long long base = (long long)(blockIdx.x - t.first_block) * MOVE_VECTORS;
+  const uint32_t block = blockIdx.x - t.first_block;
+  const long long row0 = t.block_rows > 1 ? (long long)block * t.block_rows : block / t.pieces;
+  const long long first = t.block_rows > 1 ? 0 : block % t.pieces * t.piece;   // vector of the row that the block starts at
+  const int rows = (int)(t.rows - row0 < t.block_rows ? t.rows - row0 : t.block_rows);
+  pdl_wait();
+  pdl_trigger();
+  if ((int)threadIdx.x < rows) {
+    const long long r = row0 + threadIdx.x, beams = (long long)a.B * a.W;
+    const long long i1 = r % t.n1, bw = r / t.n1 % beams, i0 = r / t.n1 / beams;
+    const int p = a.parent[bw];
+    s_from[threadIdx.x] = t.src + i0 * t.src_step[0] + i1 * t.src_step[1] + (bw / a.W * a.W + p) * t.src_row;
+    s_to[threadIdx.x] = p >= 0 && p < a.W ? t.dst + i0 * t.dst_step[0] + i1 * t.dst_step[1] + bw * t.dst_row : nullptr;
+  }
+  __syncthreads();
+  const int n = t.block_rows > 1 ? rows * (int)t.per_row : (int)(t.per_row - first < t.piece ? t.per_row - first : t.piece);
   switch (t.width) {
-    case 16: move_vectors<uint4>(t, a, base); break;
-    case 8: move_vectors<uint2>(t, a, base); break;
-    case 4: move_vectors<uint32_t>(t, a, base); break;
-    case 2: move_vectors<uint16_t>(t, a, base); break;
-    default: move_vectors<uint8_t>(t, a, base);
+    case 16: move_vectors<uint4>(t, s_from, s_to, first, n); break;
+    case 8: move_vectors<uint2>(t, s_from, s_to, first, n); break;
+    case 4: move_vectors<uint32_t>(t, s_from, s_to, first, n); break;
+    case 2: move_vectors<uint16_t>(t, s_from, s_to, first, n); break;
+    default: move_vectors<uint8_t>(t, s_from, s_to, first, n);
   }
 }
 
@@ -653,7 +683,7 @@ cudaError_t launch_beam_reorder(const q4_reorder* items, int n_items, const int3
     t.dst = static_cast<uint8_t*>(q.dst);
     t.src_row = q.src_row_step;
     t.dst_row = q.dst_row_step;
-    t.n0 = q.n[0];
+    t.rows = q.n[0] * q.n[1] * B * W;
     t.n1 = q.n[1];
     unsigned long long low = reinterpret_cast<uintptr_t>(q.src) | reinterpret_cast<uintptr_t>(q.dst) | (unsigned long long)q.row_bytes;
     if ((long long)B * W > 1) low |= (unsigned long long)(q.src_row_step | q.dst_row_step);
@@ -664,13 +694,19 @@ cudaError_t launch_beam_reorder(const q4_reorder* items, int n_items, const int3
     }
     t.width = low % 16 == 0 ? 16 : low % 8 == 0 ? 8 : low % 4 == 0 ? 4 : low % 2 == 0 ? 2 : 1;
     t.per_row = q.row_bytes / t.width;
+    const long long pieces = (t.per_row + MOVE_VECTORS - 1) / MOVE_VECTORS;
+    t.block_rows = (int)(MOVE_VECTORS / t.per_row < MOVE_ROWS ? MOVE_VECTORS / t.per_row : MOVE_ROWS);
+    if (t.block_rows < 1) t.block_rows = 1;
+    if (t.block_rows > 1) t.over = (uint32_t)((0x100000000LL + t.per_row - 1) / t.per_row);   // (not used for rows of one vector)
+    t.pieces = (unsigned)pieces;
+    t.piece = (t.per_row + pieces - 1) / pieces;
     t.first_block = (unsigned)blocks;
-    blocks += (unsigned long long)((t.n0 * t.n1 * B * W * t.per_row + MOVE_VECTORS - 1) / MOVE_VECTORS);
-    if (blocks > 0x7fffffffull) return cudaErrorInvalidValue;
+    const long long need = t.block_rows > 1 ? (t.rows + t.block_rows - 1) / t.block_rows : t.rows * pieces;
+    if (pieces > 0x7fffffff || need > 0x7fffffff || (blocks += (unsigned long long)need) > 0x7fffffffull) return cudaErrorInvalidValue;
   }
   if (blocks == 0) return cudaSuccess;
   timing_begin(s);
-  const cudaError_t e = launch_ex(k_beam_reorder, dim3((unsigned)blocks), dim3(256), 0, s, false, 1, m);
+  const cudaError_t e = launch_ex(k_beam_reorder, dim3((unsigned)blocks), dim3(MOVE_NT), 0, s, true, 1, m);
   timing_end(s);
   ++g_launches;
   return e != cudaSuccess ? e : cudaGetLastError();
