@@ -86,7 +86,8 @@ class ReorderS(C.Structure):
                 ("dst_step", C.c_int64 * 2)]
 
 
-_REORDER_ARRAYS = [ReorderS * n for n in range(REORDER_MAX + 1)]     # (making an array type takes longer than filling it)
+# arrays of n q4_reorder, field by field (a call spends less on one flat array than on structures, or on making a type)
+_REORDER_ARRAYS = [C.c_int64 * (n * C.sizeof(ReorderS) // 8) for n in range(REORDER_MAX + 1)]
 
 EXPORTS = ["q4_act_symmetric", "q4_act_asymmetric", "quantize_pack_int4", "qlstm_layer_forward",
            "qlstm_step", "q4_linear_forward", "qjoint_logprobs", "q4_beam_init",
@@ -118,7 +119,7 @@ def lib() -> C.CDLL:
         _lib.q4_rmsnorm_quantize.argtypes = [v, j, v, j, i, j, i, i, v, f, v, j, v, v, v]
         _lib.q4_linear_token_scales.argtypes = [v, v, i, C.POINTER(Mat), v, v, i, j, v, v]
         _lib.q4_lm_beam_select.argtypes = [v, j, i, v, v, i, i, i, i, f, v, v, v, v, v, v, z, v]
-        _lib.q4_beam_reorder.argtypes = [C.POINTER(ReorderS), i, v, i, i, v]
+        _lib.q4_beam_reorder.argtypes = [v, i, v, i, i, v]
     return _lib
 
 
@@ -647,15 +648,15 @@ def q4_lm_beam_select(logits: torch.Tensor, score: torch.Tensor, done: Optional[
     if (s[2] != 1 and V > 1) or (B * W > 1 and ld < V) or (B > 1 and s[0] != W * ld):
         raise ValueError("logits: contiguous rows at one distance, beams within utterances")
     stream = torch._C._cuda_getCurrentRawStream(dev)
-    arrived, scratch = _scratch_of_select(score, dev, stream, B * (W + 1), workspace_bytes(WS_LM_SELECT, (B, W, V)))
+    arrived, scratch = _scratch_of_select(score, dev, stream, B * (W + 1), _workspace_bytes(WS_LM_SELECT, (B, W, V)))
     if workspace is None:
         workspace = scratch
-    ints = score.new_empty((2, B, W), dtype=torch.int32).unbind(0)
-    out, ended = score.new_empty((B, W)), score.new_empty((B, W), dtype=torch.uint8)
+    parent, token, out = score.new_empty((3, B, W), dtype=torch.int32).unbind(0)
+    out, ended = out.view(torch.float32), score.new_empty((B, W), dtype=torch.uint8)
     _chk(lib().q4_lm_beam_select(logits.data_ptr(), max(ld, V), DTYPES[dtype], score.data_ptr(), _ptr(done), B, W, V, eos, rho,
-                                 ints[0].data_ptr(), ints[1].data_ptr(), out.data_ptr(), ended.data_ptr(), arrived.data_ptr(),
+                                 parent.data_ptr(), token.data_ptr(), out.data_ptr(), ended.data_ptr(), arrived.data_ptr(),
                                  workspace.data_ptr(), workspace.numel(), stream), "q4_lm_beam_select")
-    return {"parent": ints[0], "token": ints[1], "score": out, "done": ended}
+    return {"parent": parent, "token": token, "score": out, "done": ended}
 
 
 @functools.lru_cache(maxsize=256)
@@ -682,16 +683,15 @@ def _reorder_layout(shape: tuple, strides: tuple, es: int, dim: int, B: int, W: 
         return n, step
 
     (n0, s0), (n1, s1) = one(range(dim)), one(inner)
-    return (row_bytes if all(shape) else 0, row[0], row[1], (n0, n1), (s0[0], s1[0]), (s0[1], s1[1]))
+    return (row_bytes if all(shape) else 0, row[0], row[1], n0, n1, s0[0], s1[0], s0[1], s1[1])
 
 
-def _reorder_item(t: ReorderS, src: torch.Tensor, dst: torch.Tensor, dim: int, B: int, W: int):
+def _reorder_item(src: torch.Tensor, dst: torch.Tensor, dim: int, B: int, W: int) -> tuple:
+    """The fields of a q4_reorder, all of 64 bits, in their order."""
     shape = src.shape
     if src.dtype != dst.dtype or shape != dst.shape or shape[dim:dim + 2] != (B, W):
         raise ValueError("src and dst: alike, with utterances and beams as dimensions dim and dim + 1")
-    t.src, t.dst = src.data_ptr(), dst.data_ptr()
-    t.row_bytes, t.src_row_step, t.dst_row_step, t.n[:], t.src_step[:], t.dst_step[:] = _reorder_layout(
-        shape, (src.stride(), dst.stride()), src.element_size(), dim, B, W)
+    return (src.data_ptr(), dst.data_ptr()) + _reorder_layout(shape, (src.stride(), dst.stride()), src.element_size(), dim, B, W)
 
 
 def q4_beam_reorder(pairs: Sequence, parent: torch.Tensor, dim: int = 0):
@@ -703,12 +703,13 @@ def q4_beam_reorder(pairs: Sequence, parent: torch.Tensor, dim: int = 0):
     if dim < 0:
         raise ValueError("dim: not negative")
     B, W = parent.shape
-    dev = _on_device(parent, *(t for pair in pairs for t in pair))
+    dev = _on_device(parent, *[t for pair in pairs for t in pair])
     for first in range(0, len(pairs), REORDER_MAX):
         group = pairs[first:first + REORDER_MAX]
-        items = _REORDER_ARRAYS[len(group)]()
-        for item, (src, dst) in zip(items, group):
-            _reorder_item(item, src, dst, dim, B, W)
+        fields = ()
+        for src, dst in group:
+            fields += _reorder_item(src, dst, dim, B, W)
+        items = _REORDER_ARRAYS[len(group)](*fields)
         _chk(lib().q4_beam_reorder(items, len(group), parent.data_ptr(), B, W, torch._C._cuda_getCurrentRawStream(dev)),
              "q4_beam_reorder")
 

@@ -4,8 +4,9 @@
 //   scale = max |v| / sqrt(mean h^2 + eps) / 127,  code_i = rne(127 v_i / max |v|).
 // Codes need the row's maximum, the scale its sum of squares as well; both come from one reduction.
 //
-// Codes are those of exact arithmetic.  In fp32 t = v (127 / max |v|) is off by at most four roundings, 127 * 4 * 2^-24 < 3.1e-5; an
-// element whose t lies further than that from a half is decided by it.  The others are decided in double, where v is exact
+// Codes are those of exact arithmetic.  In fp32 t = v (127 / max |v|) is off by at most three roundings, 127 * 3 * 2^-24 < 2.3e-5; an
+// element whose t lies further than that from a half is decided by it (t is not rounded itself: a fused operation adds the number
+// that leaves its nearest integer, another takes the distance).  The others are decided in double, where v is exact
 // and a half is met exactly (`settle`); the maximum is then taken from the exact products too.
 #include <cuda_bf16.h>
 
@@ -191,6 +192,12 @@ __device__ __noinline__ void norm_row(const NormArgs& a, long long row, int t, d
 constexpr float MAGIC = 12582912.0f;   // 1.5 * 2^23: adding it leaves the nearest integer in the low bits
 constexpr float SETTLED = 0.5f - 3.2e-5f;
 
+__device__ __forceinline__ float max_abs3(float a, float b, float c) {   // of the magnitudes
+  float d;
+  asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
 __device__ __forceinline__ uint4 load_once(const void* p) {   // past the L1, which keeps the gains
   uint4 v;
   asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
@@ -294,7 +301,7 @@ __global__ void __launch_bounds__(THREADS > 128 ? THREADS : 128, norm_blocks(THR
           const uint64_t f2 = pk2(f[i], f[i + 1]);
           squares = fma2(f2, f2, squares);
           upk2(mul2(f2, pk2(g[i], g[i + 1])), v[j][i], v[j][i + 1]);
-          top = fmaxf(fmaxf(top, fabsf(v[j][i])), fabsf(v[j][i + 1]));
+          top = max_abs3(top, v[j][i], v[j][i + 1]);
         }
       }
       float odd;
@@ -308,6 +315,7 @@ __global__ void __launch_bounds__(THREADS > 128 ? THREADS : 128, norm_blocks(THR
     }
     if (t == 0) a.scale[row] = __fdiv_rn(__fdiv_rn(top, __fsqrt_rn(__fadd_rn(__fdiv_rn(sum, (float)a.k), a.eps))), 127.0f);
     const float inv = __fdiv_rn(127.0f, top);
+    const uint64_t inv2 = pk2(inv, inv), magic2 = pk2(MAGIC, MAGIC);
     uint32_t unsettled = 0;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -315,10 +323,14 @@ __global__ void __launch_bounds__(THREADS > 128 ? THREADS : 128, norm_blocks(THR
       int c[N];
       float off = 0.0f;
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float u = __fmul_rn(v[j][i], inv), m = __fadd_rn(u, MAGIC);
-        off = fmaxf(off, fabsf(__fsub_rn(u, __fsub_rn(m, MAGIC))));
-        c[i] = __float_as_int(m);
+      for (int i = 0; i < N; i += 2) {   // m = the nearest integer plus MAGIC, off: distance from it
+        const uint64_t v2 = pk2(v[j][i], v[j][i + 1]), m = fma2(v2, inv2, magic2);
+        float m0, m1, d0, d1;
+        upk2(m, m0, m1);
+        upk2(fma2(v2, inv2, sub2(magic2, m)), d0, d1);
+        off = max_abs3(off, d0, d1);
+        c[i] = __float_as_int(m0);
+        c[i + 1] = __float_as_int(m1);
       }
       if (at < a.k_pad) store_codes<N>(q + at, c);
       if (off > SETTLED) unsettled |= 1u << j;
@@ -340,8 +352,8 @@ __global__ void __launch_bounds__(THREADS > 128 ? THREADS : 128, norm_blocks(THR
       for (int i = 0; i < N; ++i) {
         const int at = (t + j * THREADS) * N + i;
         if (at >= a.k) break;
-        const float f = to_f32<T>(h[at]), g = a.gain[at], u = __fmul_rn(__fmul_rn(f, g), inv), m = __fadd_rn(u, MAGIC);
-        if (fabsf(__fsub_rn(u, __fsub_rn(m, MAGIC))) > SETTLED) q[at] = (int8_t)__double2int_rn(127.0 * ((double)f * (double)g) / exact);
+        const float f = to_f32<T>(h[at]), g = a.gain[at], p = __fmul_rn(f, g), m = __fmaf_rn(p, inv, MAGIC);
+        if (fabsf(__fmaf_rn(p, inv, __fsub_rn(MAGIC, m))) > SETTLED) q[at] = (int8_t)__double2int_rn(127.0 * ((double)f * (double)g) / exact);
       }
     }
   }

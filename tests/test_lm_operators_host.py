@@ -106,8 +106,7 @@ def test_rows_of_tensors_for_the_reordering(Bd):
              (torch.zeros(3, 4, B, W, 8), 2)]
     for src, dim in cases:
         dst = torch.zeros_like(src, memory_format=torch.contiguous_format)
-        t = Bd.ReorderS()
-        Bd._reorder_item(t, src, dst, dim, B, W)
+        t = Bd.ReorderS.from_buffer_copy((C.c_int64 * 11)(*Bd._reorder_item(src, dst, dim, B, W)))
         assert t.n[0] * t.n[1] * t.row_bytes * B * W == src.numel() * src.element_size()
         for which, x in ((0, src), (1, dst)):
             es = x.element_size()
@@ -124,13 +123,12 @@ def test_rows_of_tensors_for_the_reordering(Bd):
             who = dict(zip(at.tolist(), flat.flatten().tolist()))
             order[which] = {key: who[a] for key, a in bytes_of(t, which).items()}
         assert order[0] == order[1]
-    t = Bd.ReorderS()
     with pytest.raises(ValueError):                        # three dimensions that do not follow one another
         x = torch.zeros(B, W, 4, 4, 4, 4)[:, :, ::2, :3, ::2, :3]
-        Bd._reorder_item(t, x, torch.zeros(x.shape), 0, B, W)
+        Bd._reorder_item(x, torch.zeros(x.shape), 0, B, W)
     with pytest.raises(ValueError):
         x = torch.zeros(W, B, 4).transpose(0, 1)
-        Bd._reorder_item(t, x, torch.zeros(x.shape), 0, B, W)
+        Bd._reorder_item(x, torch.zeros(x.shape), 0, B, W)
 
 
 def test_tensors_of_other_devices_are_refused(Bd):
