@@ -545,8 +545,8 @@ int q4_encoder_recurrence_plan(int32_t T, int32_t B, int32_t dirs, int32_t H, in
                                int32_t per_sequence_scale, int32_t* out);
 
 /* Test hook for the bounded device-side waits (not an operation of the paper): while skip_producer
- * is non-zero the tiled tensor-core GEMM (the tensor-core paths of q4_linear_forward and of the
- * projections) launches with a producer that issues no copy at all, so that the consumer's wait
+ * is non-zero the tiled tensor-core GEMMs (the tensor-core paths of q4_linear_forward and of the
+ * projections, q4_linear_token_scales) launch with a producer that issues no copy at all, so that the consumer's wait
  * runs out after wait_limit polls (0 = the normal limit); nothing asynchronous is in flight, every
  * thread of the kernel still reaches its final barrier, tensor memory is freed, nothing is stored
  * and the status word reads Q4_ERR_TIMEOUT.  skip_producer = 2 has another effect: the kernel that forms a

@@ -172,6 +172,7 @@ cudaError_t launch_mma_gemm(const int8_t* x8, long long x_pitch, int M, const in
                             const float* mul_e = nullptr, const int32_t* mul_idx = nullptr,
                             const int32_t* n_idle = nullptr, int all_idle = 0);
 void test_wait_expiry_set(int skip_producer, uint32_t wait_limit);
+void test_gemm_waits(int* skip_producer, uint32_t* wait_limit);   // of mode 1
 bool test_wait_expiry_active();
 uint32_t test_ring_wait_limit();   // polls before a wait of k_state_products gives up
 cudaError_t launch_mma_gemm_i32(const int8_t* x8, int M, const int8_t* w8, int J, int K, int planes, int32_t* out,
@@ -336,8 +337,10 @@ struct TokenLinearArgs {
   long long ldo;
   int32_t M, N, K;          // K: padded row length
   int32_t* status;          // nullable
+  uint32_t wait_limit;      // polls before a wait gives up; set by the launcher
+  int32_t skip_producer;    // test hook: no copies, so the waits for them run out; set by the launcher
 };
-cudaError_t launch_token_linear(const TokenLinearArgs& a, int dtype, cudaStream_t s);
+cudaError_t launch_token_linear(TokenLinearArgs a, int dtype, cudaStream_t s);
 struct LmSelectArgs {
   const void* logits;
   long long ld;             // elements between rows

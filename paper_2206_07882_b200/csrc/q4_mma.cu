@@ -315,6 +315,10 @@ void test_wait_expiry_set(int mode, uint32_t wait_limit) {
   g_wait_limit = mode == 1 && wait_limit ? wait_limit : WAIT_LIMIT;
   g_ring_wait_limit = mode == 2 ? wait_limit : WAIT_LIMIT;
 }
+void test_gemm_waits(int* skip_producer, uint32_t* wait_limit) {
+  *skip_producer = g_skip_producer;
+  *wait_limit = g_wait_limit;
+}
 bool test_wait_expiry_active() { return g_skip_producer != 0 || g_ring_wait_limit != WAIT_LIMIT; }
 uint32_t test_ring_wait_limit() { return g_ring_wait_limit; }
 

@@ -7,7 +7,7 @@
 // Codes are those of exact arithmetic.  In fp32 t = v (127 / max |v|) is off by at most three roundings, 127 * 3 * 2^-24 < 2.3e-5; an
 // element whose t lies further than that from a half is decided by it (t is not rounded itself: a fused operation adds the number
 // that leaves its nearest integer, another takes the distance).  The others are decided in double, where v is exact
-// and a half is met exactly (`settle`); the maximum is then taken from the exact products too.
+// and a half is met exactly; the maximum is then taken from the exact products too.
 #include <cuda_bf16.h>
 
 #include "q4_internal.h"
@@ -167,6 +167,7 @@ __device__ __noinline__ void norm_row(const NormArgs& a, long long row, int t, d
   constexpr int N = Vec<T>::N;
   const T* h = a.sum ? static_cast<const T*>(a.sum) + row * a.s_ld : static_cast<const T*>(a.x) + row * a.x_ld;
   int8_t* q = a.q + row * a.k_pad;
+  __syncwarp();   // (a neighbour may have stored part of a vector of the sum; wider groups have met at a barrier since)
   double sum = 0.0, top = 0.0;
   bool bad = false;
   for (int v = t; v * N < a.k; v += THREADS)
@@ -336,6 +337,7 @@ __global__ void __launch_bounds__(THREADS > 128 ? THREADS : 128, norm_blocks(THR
       if (off > SETTLED) unsettled |= 1u << j;
     }
     if (!row_any<THREADS>(unsettled != 0)) continue;
+    __syncwarp();   // as in norm_row: elements of the sum are read again
     double exact = 0.0, unused = 0.0;
 #pragma unroll
     for (int j = 0; j < NV; ++j)

@@ -18,7 +18,6 @@ namespace {
 
 constexpr int BK = 128;        // codes per row of an operand tile
 constexpr int CH = 128;        // output channels of a CTA's tile
-constexpr uint32_t WAIT_LIMIT = 1u << 22;
 
 template <typename T> __device__ __forceinline__ T from_f32(float v);
 template <> __device__ __forceinline__ float from_f32(float v) { return v; }
@@ -110,8 +109,8 @@ k_token_linear(const __grid_constant__ CUtensorMap tma_w, const __grid_constant_
     const uint32_t on = elect_one();
     int s = 0;
     uint32_t ph = 1;
-    for (int i = 0; i < nk; ++i) {
-      ok = i < NS || mbar_wait_warp(&empty[s], ph, WAIT_LIMIT);
+    for (int i = 0; i < nk && !a.skip_producer; ++i) {
+      ok = i < NS || mbar_wait_warp(&empty[s], ph, a.wait_limit);
       if (!ok) {
         ring_landed(full, NS, i);
         break;
@@ -130,9 +129,9 @@ k_token_linear(const __grid_constant__ CUtensorMap tma_w, const __grid_constant_
     int s = 0;
     uint32_t ph = 0;
     for (int i = 0; i < nk; ++i) {
-      ok = mbar_wait_warp_tested(ready, &full[s], ph, WAIT_LIMIT);
+      ok = mbar_wait_warp_tested(ready, &full[s], ph, a.wait_limit);
       if (!ok) {
-        ring_landed(full, NS, nk);
+        if (!a.skip_producer) ring_landed(full, NS, nk);
         break;
       }
       tc_fence_after();
@@ -156,7 +155,7 @@ k_token_linear(const __grid_constant__ CUtensorMap tma_w, const __grid_constant_
   } else {
     for (int c = tid; c < TOK; c += 128) s_x[c] = m0 + c < a.M ? __ldg(a.x_scale + m0 + c) : 0.0f;
     asm volatile("bar.sync 1, 128;" ::: "memory");
-    ok = mbar_wait(&acc_full, 0, WAIT_LIMIT);
+    ok = mbar_wait(&acc_full, 0, a.wait_limit);
     ok = ok && *reinterpret_cast<volatile uint32_t*>(&failed) == 0;
     tc_fence_after();
   }
@@ -269,11 +268,11 @@ k_token_linear_pair(const __grid_constant__ CUtensorMap tma_w, const __grid_cons
     const uint32_t on = elect_one();
     int s = 0, filled = 0;
     uint32_t ph = 1;
-    for (int t = blockIdx.x / 2; t < n_tiles && ok; t += pairs) {
+    for (int t = blockIdx.x / 2; t < n_tiles && ok && !a.skip_producer; t += pairs) {
       int n0, m0;
       place(t, n0, m0);
       for (int i = 0; i < nk; ++i) {
-        ok = filled < NS || mbar_wait_warp(&empty[s], ph, WAIT_LIMIT);
+        ok = filled < NS || mbar_wait_warp(&empty[s], ph, a.wait_limit);
         if (!ok) break;
         ++filled;
         const uint32_t bar = cluster_addr(&full[s], 0);
@@ -288,7 +287,7 @@ k_token_linear_pair(const __grid_constant__ CUtensorMap tma_w, const __grid_cons
     }
     if (ok) {   // the last MMAs' arrivals on this CTA's barriers are in before it can leave
       for (int j = 0; j < min(filled, NS); ++j)
-        ok = mbar_wait_warp(&empty[j], (uint32_t)((filled - j + NS - 1) / NS - 1) & 1u, WAIT_LIMIT) && ok;
+        ok = mbar_wait_warp(&empty[j], (uint32_t)((filled - j + NS - 1) / NS - 1) & 1u, a.wait_limit) && ok;
     } else if (rank == 0) {
       ring_landed(full, NS, filled);
     }
@@ -300,12 +299,12 @@ k_token_linear_pair(const __grid_constant__ CUtensorMap tma_w, const __grid_cons
       uint32_t ph = 0;
       for (int t = blockIdx.x / 2; t < n_tiles && ok; t += pairs, ++it) {
         const int buf = it & 1, use = it >> 1;
-        if (use >= 1) ok = __all_sync(0xffffffffu, mbar_wait_cluster(&acc_empty[buf], (use - 1) & 1, WAIT_LIMIT)) != 0;
+        if (use >= 1) ok = __all_sync(0xffffffffu, mbar_wait_cluster(&acc_empty[buf], (use - 1) & 1, a.wait_limit)) != 0;
         if (!ok) break;
         tc_fence_after();
         const uint32_t d = tmem + (uint32_t)(buf * PT);
         for (int i = 0; i < nk; ++i) {
-          ok = mbar_wait_warp_tested(ready, &full[s], ph, WAIT_LIMIT);
+          ok = mbar_wait_warp_tested(ready, &full[s], ph, a.wait_limit);
           if (!ok) break;
           ++used;
           tc_fence_after();
@@ -322,7 +321,7 @@ k_token_linear_pair(const __grid_constant__ CUtensorMap tma_w, const __grid_cons
         }
         if (ok) umma_commit_pair(on, &acc_full[buf]);
       }
-      if (!ok) ring_landed(full, NS, used + NS);   // what the producers may have issued
+      if (!ok && !a.skip_producer) ring_landed(full, NS, used + NS);   // what the producers may have issued
     }
   } else {
     int it = 0;
@@ -334,7 +333,7 @@ k_token_linear_pair(const __grid_constant__ CUtensorMap tma_w, const __grid_cons
       for (int c = tid; c < PT; c += 256) s_x[buf][c] = m0 + c < a.M ? __ldg(a.x_scale + m0 + c) : 0.0f;
       const float sw = n < a.N ? __ldg(a.w_scale + n) : 0.0f, b = a.bias && n < a.N ? __ldg(a.bias + n) : 0.0f;
       asm volatile("bar.sync 1, 256;" ::: "memory");   // (nobody is still at the tile before the last, which used this buffer)
-      ok = ok && __all_sync(0xffffffffu, mbar_wait_cluster(&acc_full[buf], use & 1, WAIT_LIMIT)) != 0;
+      ok = ok && __all_sync(0xffffffffu, mbar_wait_cluster(&acc_full[buf], use & 1, a.wait_limit)) != 0;
       if (!ok) continue;                               // stores nothing any more, but meets the others at the barrier
       tc_fence_after();
       const uint32_t taddr = tmem + (uint32_t)(buf * PT + first) + ((uint32_t)(warp % 4 * 32) << 16);
@@ -448,7 +447,8 @@ cudaError_t launch_typed(const TokenLinearArgs& a, cudaStream_t s) {
 
 }  // namespace
 
-cudaError_t launch_token_linear(const TokenLinearArgs& a, int dtype, cudaStream_t s) {
+cudaError_t launch_token_linear(TokenLinearArgs a, int dtype, cudaStream_t s) {
+  test_gemm_waits(&a.skip_producer, &a.wait_limit);
   timing_begin(s);
   const cudaError_t e = dtype == Q4_F32   ? launch_typed<float>(a, s)
                         : dtype == Q4_F16 ? launch_typed<__half>(a, s)

@@ -1,5 +1,6 @@
 """The operators around a language model's output against plain 64-bit computations of the same formulas: norm with 8-bit
 codes, linear layer with token scales, beam selection over a vocabulary, reordering of states."""
+import ctypes as C
 import math
 
 import numpy as np
@@ -190,6 +191,26 @@ def test_linear_of_the_longest_rows(Bd, M):
     x[:] = -128
     w[0], w[1] = -128, 127
     check_linear(Bd, x, w, sx, sw, None, torch.float32)
+
+
+@pytest.mark.parametrize("M,N,K", [(5, 300, 256), (16, 256, 4096), (100, 700, 300), (1024, 4096, 256)])
+def test_linear_whose_wait_runs_out_stores_nothing(Bd, M, N, K):
+    # one tile a CTA, a split, wider tiles, pairs of CTAs: the producers issue no copy, every thread leaves, the status says so
+    x, w, sx, sw, b = linear_inputs(M, N, K, 11)
+    lin = Bd.DeviceLinear.from_mat(Bd.DeviceMat(w.cuda().view(torch.uint8), sw.cuda(), N, w.shape[1], w.shape[1], 8), b.cuda())
+    out, status = torch.full((M, N), 3.0, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    xd, sxd = x.cuda().view(torch.uint8), sx.cuda()
+    assert Bd.lib().q4_test_wait_expiry_set(C.c_int32(1), C.c_uint32(1 << 12)) == 0
+    try:
+        Bd.q4_linear_token_scales(xd, sxd, lin, out=out, status=status)
+        assert Bd.q4_poll_status(status) == -8
+    finally:
+        Bd.lib().q4_test_wait_expiry_set(C.c_int32(0), C.c_uint32(0))
+    assert (out == 3.0).all()
+    status.zero_()
+    Bd.q4_linear_token_scales(xd, sxd, lin, out=out, status=status)
+    assert Bd.q4_poll_status(status) == 0
+    assert torch.equal(out, Bd.q4_linear_token_scales(xd, sxd, lin)) and not (out == 3.0).all()
 
 
 def test_linear_rows_without_a_scale_stay_alone(Bd):
