@@ -236,17 +236,21 @@ __device__ __forceinline__ void pack(Vec<__nv_bfloat16>& v, const float (&f)[8])
   }
 }
 
-// A row per group of THREADS threads, 128 or THREADS threads a block; everything is read and written once, the products v lie in
-// registers, NV vectors of 16 bytes of the row a thread.  WHOLE: rows are 16-byte aligned and a multiple of that long.
-// Bound by memory.  One warp a row needs no barrier; wider groups take rows that a warp's registers do not hold, and few rows,
-// where a row's latency is the call's.
-// blocks of an SM: 64 registers a thread for up to 16 elements, 80 for up to 32, 96 and 128 for up to 48 and 64
+// A row per group of THREADS threads; everything is read and written once, the products v lie in registers, NV vectors of 16 bytes of
+// the row a thread.  WHOLE: rows are 16-byte aligned and a multiple of that long.
+// Long rows are bound by memory (4096 x 4096 with a residual: fp32 36.9 us, 5.9 TB/s; bf16 24.4 us, 4.8 TB/s), short ones of 16 bits
+// by their instructions, about 16 for each element (16000 x 1280 fp16 alone: 20.1 us, 3.1 TB/s).  One warp a row needs no barrier; wider
+// groups take rows that a warp's registers do not hold, and few rows, where a row's latency is the call's (16 x 1024: 2.2 us).
+// Forming the products again for the codes, for registers of half as many bits, took 10 % more.  Rows that are not 16-byte
+// aligned (4096 x 4001 bf16) take 49 us; element by element they took 75.
+// Threads of a block: four rows of one warp, or one row.  Blocks of an SM: 64 registers a thread for up to 16 elements, 80 for up to 32, 96 and 128 for up to 48 and 64
+__host__ __device__ constexpr int norm_threads(int threads) { return threads > 32 ? threads : 128; }
 __host__ __device__ constexpr int norm_blocks(int threads, int elements) {
-  return 128 * (elements <= 16 ? 8 : elements <= 32 ? 6 : elements <= 48 ? 5 : 4) / (threads > 128 ? threads : 128);
+  return 128 * (elements <= 16 ? 8 : elements <= 32 ? 6 : elements <= 48 ? 5 : 4) / norm_threads(threads);
 }
 template <typename T, int THREADS, int NV, bool WHOLE>
-__global__ void __launch_bounds__(THREADS > 128 ? THREADS : 128, norm_blocks(THREADS, NV * (16 / (int)sizeof(T)))) k_rmsnorm_quantize(const __grid_constant__ NormArgs a) {
-  constexpr int N = Vec<T>::N, ROWS = THREADS >= 128 ? 1 : 128 / THREADS;
+__global__ void __launch_bounds__(norm_threads(THREADS), norm_blocks(THREADS, NV * (16 / (int)sizeof(T)))) k_rmsnorm_quantize(const __grid_constant__ NormArgs a) {
+  constexpr int N = Vec<T>::N, ROWS = norm_threads(THREADS) / THREADS;
   __shared__ float s_part[THREADS / 32][2];
   __shared__ double s_part64[THREADS / 32][2];
   const int t = threadIdx.x % THREADS;
@@ -381,10 +385,10 @@ __global__ void __launch_bounds__(512) k_rmsnorm_quantize_long(const __grid_cons
 
 template <typename T, int THREADS, int NV>
 cudaError_t launch_rows(const NormArgs& a, bool whole, cudaStream_t s) {
-  constexpr int ROWS = THREADS >= 128 ? 1 : 128 / THREADS;
+  constexpr int ROWS = norm_threads(THREADS) / THREADS;
   const long long blocks = (a.rows + ROWS - 1) / ROWS;
   return launch_ex(whole ? k_rmsnorm_quantize<T, THREADS, NV, true> : k_rmsnorm_quantize<T, THREADS, NV, false>,
-                   dim3((unsigned)(blocks < (1 << 20) ? blocks : 1 << 20)), dim3(THREADS > 128 ? THREADS : 128), 0, s, true, 1, a);
+                   dim3((unsigned)(blocks < (1 << 20) ? blocks : 1 << 20)), dim3(norm_threads(THREADS)), 0, s, true, 1, a);
 }
 template <typename T>
 cudaError_t launch_norm(const NormArgs& a, cudaStream_t s) {
@@ -394,12 +398,13 @@ cudaError_t launch_norm(const NormArgs& a, cudaStream_t s) {
   const bool whole = low % 16 == 0;
   const int vectors = a.k_pad / Vec<T>::N;
   constexpr int MOST = 32 / Vec<T>::N;      // vectors of a thread in wide groups: 32 elements in registers
-  // Many rows: the narrowest group that holds a row.  Few (less than 16 for each SM): no more than two vectors a thread.
+  // Many rows: the narrowest group that holds a row (3000 x 2048 fp16: 64 threads 8.0 us, a warp 9.7; 16000 x 1280: 21.9 and 20.1).
+  // Few (less than 16 for each SM): no more than two vectors a thread.
   if (a.rows >= 16LL * sm_count()) {
     if (vectors <= 32 * 2) return launch_rows<T, 32, 2>(a, whole, s);
     if (vectors <= 32 * 4) return launch_rows<T, 32, 4>(a, whole, s);
     if (vectors <= 32 * 6) return launch_rows<T, 32, 6>(a, whole, s);
-    if (vectors <= 32 * 8) return launch_rows<T, 32, 8>(a, whole, s);
+    if (vectors <= 64 * 4) return launch_rows<T, 64, 4>(a, whole, s);
     if (vectors <= 128 * MOST) return launch_rows<T, 128, MOST>(a, whole, s);
     if (vectors <= 256 * MOST) return launch_rows<T, 256, MOST>(a, whole, s);
   }
