@@ -2014,6 +2014,7 @@ int q4_beam_reorder(const q4_reorder* items, int32_t n_items, const int32_t* par
     if (rows > 1 && t.dst_row_step < t.row_bytes) return Q4_ERR_DIM;
     for (int d = 0; d < 2; ++d)
       if (t.src_step[d] < 0 || t.dst_step[d] < 0 || (t.n[d] > 1 && t.dst_step[d] < t.row_bytes)) return Q4_ERR_DIM;
+    if ((__int128)t.n[0] * t.n[1] > ((int64_t)1 << 47) / rows) return Q4_ERR_DIM;   // (rows of dst lie apart)
     if (!reorder_extent(t.src, t, t.src_row_step, t.src_step, rows, &lo[0][i], &hi[0][i]) ||
         !reorder_extent(t.dst, t, t.dst_row_step, t.dst_step, rows, &lo[1][i], &hi[1][i]))
       return Q4_ERR_DIM;

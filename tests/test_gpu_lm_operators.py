@@ -516,6 +516,36 @@ def test_steps_on_two_streams_at_once(Bd):
             assert all(torch.equal(r[k], want[i][k]) for k in want[i])
 
 
+def far_rows(t, step):
+    """t [rows, k] on the device with rows `step` elements apart (more than 2^31 in all), what lies between them unread."""
+    big = torch.empty((t.shape[0] - 1) * step + t.shape[1], dtype=t.dtype, device="cuda")
+    view = big.as_strided(t.shape, (step, 1))
+    view.copy_(t)
+    return view
+
+
+def test_rows_further_apart_than_32_bits_count(Bd):
+    g, step = gen(12), (1 << 30) + 40
+    x = torch.randn(4, 96, generator=g).to(torch.float16)
+    codes, scale = Bd.q4_rmsnorm_quantize(far_rows(x, step), torch.ones(96, device="cuda"), 1e-5)
+    _, want, want_scale = norm_oracle(x, torch.ones(96), 1e-5)
+    assert torch.equal(codes.cpu().view(torch.int8).double(), want)
+    xi, w, sx, sw, _ = linear_inputs(4, 100, 96, 3, bias=False)
+    lin = Bd.DeviceLinear.from_mat(Bd.DeviceMat(w.cuda().view(torch.uint8), sw.cuda(), 100, 96, 96, 8))
+    out = far_rows(torch.zeros(4, 100, dtype=torch.float16), step)
+    Bd.q4_linear_token_scales(xi.cuda().view(torch.uint8), sx.cuda(), lin, out=out)
+    assert torch.equal(out.clone(), Bd.q4_linear_token_scales(xi.cuda().view(torch.uint8), sx.cuda(), lin, out_dtype=torch.float16))
+    logits = torch.randn(1, 4, 300, generator=g).to(torch.float16)
+    score = torch.randn(1, 4, generator=g)
+    far = far_rows(logits[0], step).as_strided((1, 4, 300), (4 * step, step, 1))
+    near, got = Bd.q4_lm_beam_select(logits.cuda(), score.cuda()), Bd.q4_lm_beam_select(far, score.cuda())
+    assert all(torch.equal(near[k], got[k]) for k in near)
+    rows = torch.randn(4, 50, generator=g).to(torch.float16)
+    src, dst = far_rows(rows, step).as_strided((1, 4, 50), (4 * step, step, 1)), torch.zeros(1, 4, 50, dtype=torch.float16, device="cuda")
+    Bd.q4_beam_reorder([(src, dst)], torch.tensor([[3, 2, -1, 0]], dtype=torch.int32, device="cuda"))
+    assert torch.equal(dst[0].cpu(), torch.stack([rows[3], rows[2], 0 * rows[0], rows[0]]))
+
+
 # -------------------------------------------------------------------------------------------------------- refusals
 def test_refusals_of_the_binding(Bd):
     x = torch.randn(4, 64, device="cuda")

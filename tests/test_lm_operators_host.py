@@ -86,6 +86,7 @@ def test_reorder_refusals(Bd):
     assert call(item(row=-1)) == -2 and call(item(ss=-64)) == -2 and call(item(ds=63)) == -2
     assert call(item(n=(-1, 1))) == -2 and call(item(n=(2, 1), s=(512, 0), d=(63, 0))) == -2
     assert call(item(n=(1 << 40, 1), s=(1 << 40, 0), d=(1 << 40, 0))) == -2
+    assert call(item(n=(1 << 32, 1 << 32), row=1, ss=1, ds=1, s=(1, 1), d=(1, 1))) == -2   # more rows than addresses
     assert call(item(dst=1 << 20)) == -6                                       # in place
     assert call(item(dst=(1 << 20) + 7 * 64 + 63)) == -6                       # the last byte of the last row
     assert call(item(), item(src=1 << 21, dst=1 << 22)) == -6                  # one tensor's new rows are another's old ones
