@@ -82,6 +82,24 @@ def test_norm(Bd, dtype, rows, k, gap, with_residual):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,k,k_pad", [(3, 1, 64), (5000, 33, 160), (2500, 640, 1024), (4, 4000, 4096), (2400, 2049, 2112)])
+def test_norm_into_longer_rows(Bd, dtype, rows, k, k_pad):
+    # few and many rows (a row on a warp, on two, on more), with codes of 0 behind them
+    g = gen(k)
+    x, r = (torch.randn(rows, k, generator=g).to(dtype) for _ in range(2))
+    check_norm(Bd, x, torch.randn(k, generator=g), residual=r, k_pad=k_pad)
+    check_norm(Bd, x, torch.randn(k, generator=g), gap=8 - k % 8, k_pad=k_pad)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,k", [(2400, 1536), (2400, 2048), (2500, 4096), (2400, 8000), (2400, 1537)])
+def test_norm_of_many_rows(Bd, dtype, rows, k):
+    g = gen(k)
+    x, r = (torch.randn(rows, k, generator=g).to(dtype) for _ in range(2))
+    check_norm(Bd, x, torch.randn(k, generator=g), residual=r)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("k", [64, 1003, 9001])
 def test_norm_of_values_next_to_a_half(Bd, dtype, k):
     # a row maximum of 127 (or 254) makes many quotients exact halves, which go to the even neighbour
