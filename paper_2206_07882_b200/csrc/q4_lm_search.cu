@@ -49,6 +49,11 @@ struct RowParts {
 // (value, label) a before b
 __device__ __forceinline__ bool before(float va, int la, float vb, int lb) { return va > vb || (va == vb && la < lb); }
 
+__device__ __forceinline__ uint4 load_once(const uint4* p) {   // past the L1: 4 % of a call
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
 template <typename T> struct Vec;
 template <> struct Vec<float> {
   static constexpr int N = 4;
@@ -113,6 +118,8 @@ __device__ __forceinline__ long long order_key(double c) {
   const long long b = __double_as_longlong(c + 0.0);       // (-0 becomes 0)
   return b >= 0 ? b : b ^ 0x7fffffffffffffffLL;
 }
+// the keys of -+(2 - 2^-24) 2^127: scores between them are finite in fp32
+constexpr long long LOWEST_SCORE = (long long)0xB81000000FFFFFFFULL, HIGHEST_SCORE = 0x47EFFFFFF0000000LL;
 __device__ __forceinline__ double key_score(long long k) { return __longlong_as_double(k >= 0 ? k : k ^ 0x7fffffffffffffffLL); }
 __device__ __forceinline__ bool before(const Proposal& a, const Proposal& b) {
   return a.key > b.key || (a.key == b.key && (a.beam < b.beam || (a.beam == b.beam && before(a.z, a.label, b.z, b.label))));
@@ -125,11 +132,11 @@ struct RowShared {            // of a segment
   int32_t label[ROW_LIST];
 };
 struct MergeShared {
-  double score[MAX_BEAMS], lse[MAX_BEAMS];   // lse NaN: the beam proposes nothing
-  int32_t ended[MAX_BEAMS];
+  double base[MAX_BEAMS], lse[MAX_BEAMS];   // score + rho and log-sum-exp of a beam's row; an ended beam's score
+  int32_t kind[MAX_BEAMS];                  // 0: the beam proposes nothing, 1: labels, 2: it has ended
   long long key[MERGE_LIST];
   float z[MERGE_LIST];
-  int32_t label[MERGE_LIST], beam[MERGE_LIST];
+  int32_t label[MERGE_LIST], beam[MERGE_LIST], pick[MERGE_LIST];
 };
 struct SelectShared {
   union {
@@ -139,7 +146,7 @@ struct SelectShared {
   Best best[ROW_NT / 32];
   double sum[ROW_NT / 32];
   float group[ROW_GROUPS], top[ROW_NT / 32], scale[ROW_NT / 32], bound[2];
-  int32_t noted, n, last;
+  int32_t noted, n, picked, last;
 };
 static_assert(sizeof(SelectShared) * ROW_BLOCKS <= 200 * 1024, "shared memory of an SM");
 
@@ -250,10 +257,10 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
   auto fetch = [&](uint4 (&raw)[ROW_VECTORS]) {
     if (left > (ROW_VECTORS - 1) * ROW_NT) {
 #pragma unroll
-      for (int j = 0; j < ROW_VECTORS; ++j) raw[j] = __ldg(src + j * ROW_NT);
+      for (int j = 0; j < ROW_VECTORS; ++j) raw[j] = load_once(src + j * ROW_NT);
     } else {
 #pragma unroll
-      for (int j = 0; j < ROW_VECTORS; ++j) raw[j] = j * ROW_NT < left ? __ldg(src + j * ROW_NT) : lowest_vector<T>();
+      for (int j = 0; j < ROW_VECTORS; ++j) raw[j] = j * ROW_NT < left ? load_once(src + j * ROW_NT) : lowest_vector<T>();
     }
     src += ROW_TURN;
     left -= ROW_TURN;
@@ -437,60 +444,72 @@ __device__ __forceinline__ void merge_row(const RowParts& p, long long row, int 
   }
 }
 
-// The W best proposals of an utterance from its rows' lists.  A proposal's score is score[w] + (z - lse + rho) in double.  As for a
-// segment a bound from group maxima (rounded down to fp32, so it errs on the safe side) leaves few proposals to rank.
+// The W best proposals of an utterance from its rows' lists.  A proposal's score is score[w] + rho + (z - lse) in double (the logits may
+// be far larger than their differences).  As for a segment a bound from group maxima (rounded down to fp32, so it errs on
+// the safe side) leaves few proposals to rank; where the best are in few groups (beams far apart, or many beams alike) it leaves
+// hundreds, and a second bound is taken among those.
+// Double precision is slow to wait for: two additions and two conversions an entry, everything else is done on the keys.
 __device__ __forceinline__ void merge_rows(const LmSelectArgs& a, const RowParts& p, int utterance, SelectShared& sh) {
   MergeShared& mg = sh.merge;
   const int tid = threadIdx.x, W = a.W, entries = W * W;   // entry w W + j: place j of beam w
   const long long row0 = (long long)utterance * W;
+  const int over = 65536 / W + 1;                          // e / W = e over >> 16 for e < 1024
   constexpr int EACH = MERGE_LIST / ROW_NT;
   Best mine[EACH];
 #pragma unroll
   for (int i = 0; i < EACH; ++i) {
-    const int e = tid + i * ROW_NT;
-    mine[i] = e < entries ? load_best(p.best + (row0 + e / W) * p.parts * W + e % W) : Best{-INFINITY, -1};
+    const int e = tid + i * ROW_NT, w = e * over >> 16;
+    mine[i] = e < entries ? load_best(p.best + (row0 + w) * p.parts * W + (e - w * W)) : Best{-INFINITY, -1};
   }
   if (tid < W) {
     const float score = a.score[row0 + tid];
     const bool ended = a.done && a.done[row0 + tid] && isfinite(score);
     const double lse = __ldcg(p.lse + (row0 + tid) * p.parts);              // (a beam that is empty or ended left none: not used)
-    mg.score[tid] = score;
-    mg.lse[tid] = isfinite(score) && !ended && isfinite(lse) ? lse : NAN;   // (not finite: nothing but -inf, a NaN or +inf)
-    mg.ended[tid] = ended;
+    const bool rows = isfinite(score) && !ended && isfinite(lse);           // (not finite: nothing but -inf, a NaN or +inf)
+    mg.base[tid] = ended ? (double)score : (double)score + (double)a.rho;
+    mg.lse[tid] = lse;
+    mg.kind[tid] = ended ? 2 : rows ? 1 : 0;
   }
-  if (tid == 0) sh.n = 0;
+  if (tid == 0) sh.n = sh.picked = 0;
   __syncthreads();
-  auto proposal = [&](int e, const Best& b) {
-    const int w = e / W;
-    Proposal q{NO_PROPOSAL, -INFINITY, -1, w};
-    if (e >= entries) return q;
-    if (mg.ended[w]) {
-      if (e == w * W) q = Proposal{order_key(mg.score[w]), 0.0f, a.eos, w};
-    } else if (!isnan(mg.lse[w]) && b.label >= 0) {
-      const double c = mg.score[w] + (((double)b.value - mg.lse[w]) + (double)a.rho);
-      if (isfinite((float)c)) q = Proposal{order_key(c), b.value, b.label, w};
+  long long key[EACH], head = NO_PROPOSAL;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    const int e = tid + i * ROW_NT, w = e * over >> 16;
+    key[i] = NO_PROPOSAL;
+    if (e >= entries) continue;
+    const int kind = mg.kind[w];
+    if (kind == 1 && mine[i].label >= 0) {
+      const long long k = order_key(mg.base[w] + ((double)mine[i].value - mg.lse[w]));
+      if (k > LOWEST_SCORE && k < HIGHEST_SCORE) key[i] = k;
+    } else if (kind == 2 && e == w * W) {
+      key[i] = order_key(mg.base[w]);
+      mine[i] = Best{0.0f, a.eos};
     }
-    return q;
-  };
-  long long head = NO_PROPOSAL;
+    head = max(head, key[i]);
+  }
+  long long bound = order_key((double)group_bound(sh, __double2float_rd(key_score(head)), W));
 #pragma unroll
   for (int i = 0; i < EACH; ++i)
-    if (i * ROW_NT < entries) head = max(head, proposal(tid + i * ROW_NT, mine[i]).key);
-  const long long bound = order_key((double)group_bound(sh, __double2float_rd(key_score(head)), W));
-#pragma unroll
-  for (int i = 0; i < EACH; ++i)
-    if (i * ROW_NT < entries) {
-      const Proposal q = proposal(tid + i * ROW_NT, mine[i]);
-      if (q.key > NO_PROPOSAL && q.key >= bound) {
-        const int at = atomicAdd(&sh.n, 1);
-        mg.key[at] = q.key;
-        mg.z[at] = q.z;
-        mg.label[at] = q.label;
-        mg.beam[at] = q.beam;
-      }
+    if (key[i] > NO_PROPOSAL && key[i] >= bound) {
+      const int at = atomicAdd(&sh.n, 1);
+      mg.key[at] = key[i];
+      mg.z[at] = mine[i].value;
+      mg.label[at] = mine[i].label;
+      mg.beam[at] = (tid + i * ROW_NT) * over >> 16;
     }
   __syncthreads();
-  const int n = sh.n;
+  int n = sh.n;
+  const bool many = n > ROW_NT;
+  if (many) {
+    head = NO_PROPOSAL;
+    for (int i = tid; i < n; i += ROW_NT) head = max(head, mg.key[i]);
+    bound = order_key((double)group_bound(sh, __double2float_rd(key_score(head)), W));
+    for (int i = tid; i < n; i += ROW_NT)
+      if (mg.key[i] >= bound) mg.pick[atomicAdd(&sh.picked, 1)] = i;
+    __syncthreads();
+    n = sh.picked;
+  }
   auto store = [&](int i, const Proposal& q, bool some) {
     const long long o = row0 + i;
     a.parent[o] = some ? q.beam : -1;
@@ -498,35 +517,36 @@ __device__ __forceinline__ void merge_rows(const LmSelectArgs& a, const RowParts
     a.score_out[o] = some ? (float)key_score(q.key) : -INFINITY;
     if (a.done_out) a.done_out[o] = some && q.label == a.eos;
   };
+  auto place = [&](int i) { return many ? mg.pick[i] : i; };
   auto listed = [&](int i) { return Proposal{mg.key[i], mg.z[i], mg.label[i], mg.beam[i]}; };
   for (int i = tid; i < max(n, W); i += ROW_NT) {
     if (i >= n) {
       store(i, Proposal{}, false);
       continue;
     }
-    const Proposal q = listed(i);
+    const Proposal q = listed(place(i));
     int rank = 0, equal = 0;
 #pragma unroll 8
     for (int j = 0; j < n; ++j) {
-      const long long k = mg.key[j];
+      const long long k = mg.key[place(j)];
       rank += k > q.key;
       equal += k == q.key;
     }
     if (rank < W && equal > 1)
-      for (int j = 0; j < n; ++j) rank += mg.key[j] == q.key && before(listed(j), q);
+      for (int j = 0; j < n; ++j) rank += mg.key[place(j)] == q.key && before(listed(place(j)), q);
     if (rank < W) store(rank, q, true);
   }
 }
 
 // One block per segment; the last of a row's blocks to be through merges the row, the last of an utterance's rows the utterance.
-// A block that arrives publishes what its threads wrote (a barrier and a fence before the count), the last one reads the others' after
-// the count and a fence, past the L1.  The counts wrap to 0 for the next call.
+// A block that arrives publishes what its threads wrote (a barrier, then a releasing count), the last one reads the others' after
+// the count, which acquires, past the L1.  The counts wrap to 0 for the next call.
 __device__ __forceinline__ bool last_to_arrive(uint32_t* count, uint32_t of, SelectShared& sh) {
   __syncthreads();
   if (threadIdx.x == 0) {
-    __threadfence();
-    sh.last = atomicInc(count, of - 1) == of - 1;
-    __threadfence();
+    uint32_t before;
+    asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;" : "=r"(before) : "l"(count), "r"(of - 1) : "memory");
+    sh.last = before == of - 1;
   }
   __syncthreads();
   return sh.last != 0;
