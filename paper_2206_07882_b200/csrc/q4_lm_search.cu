@@ -444,6 +444,9 @@ __device__ __forceinline__ void merge_row(const RowParts& p, long long row, int 
   }
 }
 
+// How far sums of the same row may lie apart (terms off by 2^-22, chains of 64 roundings)
+constexpr double SAME_SUM = 4.2e-6;
+
 // The W best proposals of an utterance from its rows' lists.  A proposal's score is score[w] + rho + (z - lse) in double (the logits may
 // be far larger than their differences).  As for a segment a bound from group maxima (rounded down to fp32, so it errs on
 // the safe side) leaves few proposals to rank; where the best are in few groups (beams far apart, or many beams alike) it leaves
@@ -461,14 +464,35 @@ __device__ __forceinline__ void merge_rows(const LmSelectArgs& a, const RowParts
     const int e = tid + i * ROW_NT, w = e * over >> 16;
     mine[i] = e < entries ? load_best(p.best + (row0 + w) * p.parts * W + (e - w * W)) : Best{-INFINITY, -1};
   }
-  if (tid < W) {
-    const float score = a.score[row0 + tid];
-    const bool ended = a.done && a.done[row0 + tid] && isfinite(score);
-    const double lse = __ldcg(p.lse + (row0 + tid) * p.parts);              // (a beam that is empty or ended left none: not used)
+  if (tid < 32) {
+    const float score = tid < W ? a.score[row0 + tid] : -INFINITY;
+    const bool ended = tid < W && a.done && a.done[row0 + tid] && isfinite(score);
+    double lse = tid < W ? __ldcg(p.lse + (row0 + tid) * p.parts) : NAN;    // (a beam that is empty or ended left none: not used)
     const bool rows = isfinite(score) && !ended && isfinite(lse);           // (not finite: nothing but -inf, a NaN or +inf)
-    mg.base[tid] = ended ? (double)score : (double)score + (double)a.rho;
-    mg.lse[tid] = lse;
-    mg.kind[tid] = ended ? 2 : rows ? 1 : 0;
+    // Beams of equal scores and equal rows have equal proposals, but rows that begin at different places of 16 bytes are summed in
+    // another order.  Such a beam takes the sum of the first one like it: same score, same list, and all but the same sum.
+    uint32_t like = __match_any_sync(0xffffffffu, rows ? __float_as_uint(score + 0.0f) : 0x7fc00000u | tid) & ((1u << tid) - 1);
+    const double own = lse;
+    while (__any_sync(0xffffffffu, like != 0)) {
+      const int w = like ? __ffs(like) - 1 : tid;
+      const double other = __shfl_sync(0xffffffffu, own, w);
+      if (like == 0) continue;
+      like &= like - 1;
+      if (!(fabs(own - other) <= SAME_SUM)) continue;
+      int j = 0;
+      for (; j < W; ++j) {
+        const Best mine_j = load_best(p.best + (row0 + tid) * p.parts * W + j), other_j = load_best(p.best + (row0 + w) * p.parts * W + j);
+        if (mine_j.value != other_j.value || mine_j.label != other_j.label) break;
+      }
+      if (j < W) continue;
+      lse = other;
+      like = 0;
+    }
+    if (tid < W) {
+      mg.base[tid] = ended ? (double)score : (double)score + (double)a.rho;
+      mg.lse[tid] = lse;
+      mg.kind[tid] = ended ? 2 : rows ? 1 : 0;
+    }
   }
   if (tid == 0) sh.n = sh.picked = 0;
   __syncthreads();

@@ -316,6 +316,19 @@ def test_select(Bd, B, W, V, dtype):
         check_select(Bd, logits, score, done=done.to(torch.uint8), eos=V // 2, gap=1)
 
 
+@pytest.mark.parametrize("V", [3, 41, 1001, 9001, 50257])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_select_of_equal_beams_in_rows_that_begin_anywhere(Bd, V, dtype):
+    # equal beams of equal scores are told apart by their number alone, wherever their rows begin in memory
+    g, W = gen(V), 12
+    row, other = torch.randn(V, generator=g).to(dtype), torch.randn(V, generator=g).to(dtype)
+    logits = torch.stack([row, other, row, row, other, row, row, other, row, row, other, row])[None].contiguous()
+    score = torch.tensor([[0.0, 0.1, 0.0, 0.0, 0.1, -0.0, 0.0, 0.1, -0.25, -0.25, 0.1, 0.0]])
+    for gap in (0, 1, 2):
+        check_select(Bd, logits, score, gap=gap)
+        check_select(Bd, logits, torch.zeros(1, W), gap=gap, rho=0.5)
+
+
 @pytest.mark.parametrize("V", [40, 1024, 9000, 40000])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_select_of_equal_and_ordered_logits(Bd, V, dtype):
@@ -532,6 +545,52 @@ def test_steps_on_two_streams_at_once(Bd):
     for i in range(2):
         for r in got[i]:
             assert all(torch.equal(r[k], want[i][k]) for k in want[i])
+
+
+def shifted(t, at, gap):
+    """t on the device as columns `at` and on of a wider tensor that is NaN elsewhere."""
+    wide = torch.full(t.shape[:-1] + (at + t.shape[-1] + gap,), NAN, dtype=t.dtype)
+    wide[..., at:at + t.shape[-1]] = t
+    return wide.cuda()[..., at:at + t.shape[-1]]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("at", [1, 2, 3, 5, 7])
+def test_views_that_begin_anywhere(Bd, dtype, at):
+    # rows that begin at every place of a 16-byte granule, the first and the last element of a tensor among them
+    g = gen(at)
+    for rows, k in ((6, 777), (2500, 200), (3, 5), (2400, 1029)):
+        x, r = (torch.randn(rows, k, generator=g).to(dtype) for _ in range(2))
+        gain = torch.randn(k, generator=g)
+        h, want, want_scale = norm_oracle(x, gain, 1e-5, r)
+        for gap in (0, 1, 8):
+            xd, rd, sd = shifted(x, at, gap), shifted(r, at + 1, gap), shifted(torch.zeros_like(x), 2 * at, gap + 1)
+            codes, scale = Bd.q4_rmsnorm_quantize(xd, gain.cuda(), 1e-5, residual=rd, sum_out=sd)
+            assert torch.equal(codes.cpu().view(torch.int8)[:, :k].double(), want) and torch.equal(sd.cpu(), h)
+            np.testing.assert_allclose(scale.cpu().double().numpy(), want_scale.numpy(), rtol=SCALE_RTOL, atol=0)
+            whole = sd.as_strided((rows, k + 2 * at + gap + 1), (k + 2 * at + gap + 1, 1), 0).cpu()
+            assert whole[:, :2 * at].isnan().all() and whole[:, 2 * at + k:].isnan().all()
+            Bd.q4_rmsnorm_quantize(xd, gain.cuda(), 1e-5, residual=rd, sum_out=rd)      # in place
+            assert torch.equal(rd.cpu(), h)
+    for B, W, V in ((2, 5, 1003), (1, 3, 6), (3, 16, 20011)):
+        logits, score = torch.randn(B, W, V, generator=g).to(dtype), torch.randn(B, W, generator=g)
+        near = Bd.q4_lm_beam_select(logits.cuda(), score.cuda())
+        for gap in (0, 3):
+            got = Bd.q4_lm_beam_select(shifted(logits, at, gap), score.cuda())
+            assert all(torch.equal(near[n], got[n]) for n in ("parent", "token", "done"))
+            # a row that begins elsewhere is summed in another order: each sum within LSE_TOL, a score rounded once
+            assert ((near["score"] - got["score"]).abs() <= 2 * LSE_TOL + 2.0 ** -23 * near["score"].abs()).all()
+    x, w, sx, sw, b = linear_inputs(70, 333, 96, at)
+    lin = Bd.DeviceLinear.from_mat(Bd.DeviceMat(w.cuda().view(torch.uint8), sw.cuda(), 333, 96, 96, 8), b.cuda())
+    want = Bd.q4_linear_token_scales(x.cuda().view(torch.uint8), sx.cuda(), lin, out_dtype=dtype)
+    out = shifted(torch.zeros(70, 333, dtype=dtype), at, 2)
+    Bd.q4_linear_token_scales(x.cuda().view(torch.uint8), sx.cuda(), lin, out=out)
+    assert torch.equal(out, want)
+    src, dst = torch.randn(2, 4, 37, generator=g).to(dtype), torch.randn(2, 4, 37, generator=g).to(dtype)
+    parent = parents(2, 4, at)
+    to = shifted(dst, 2 * at, 1)
+    Bd.q4_beam_reorder([(shifted(src, at, 3), to)], parent.cuda())
+    assert torch.equal(to.cpu(), reorder_oracle(src, dst, parent, 0))
 
 
 def far_rows(t, step):
