@@ -237,7 +237,7 @@ __device__ __forceinline__ void best_by_passes(SelectShared& sh, F get, int from
 // 45 (W = 32) elements pass between two bounds.  The noted vectors' elements that reach the last bound are ranked.  More than the
 // lists take (equal or rising logits) are given up for W passes over the segment.
 // The next turn's vectors are on their way into registers while a turn is worked on: 56 KB in the seven blocks of an SM.
-// Bound by memory: 64 x 16 rows of 32000 fp32 logits, 131 MB, take 31 us with a fifth of the beams ended; a kernel that only
+// Bound by memory: 64 x 16 rows of 32000 fp32 logits, 131 MB, take 28 us with a fifth of the beams ended; a kernel that only
 // reads 134 MB in blocks like these takes 25 us, in the best of blocks 23.  Tried at 64 x 16 x 32768: candidates read again once the last
 // bound was known 14 us more, one bound of the first turn 9 us more, two turns ahead by asynchronous copies to shared memory no
 // gain, five blocks with twice the vectors 6 us more (two waves of blocks).
