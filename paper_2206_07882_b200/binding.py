@@ -588,9 +588,9 @@ def q4_linear_token_scales(xq: torch.Tensor, x_scale: torch.Tensor, lin: DeviceL
     _need_cuda()
     w = lin.w
     dev = _on_device(xq, x_scale, w.q, out, status)
-    if xq.dim() != 2 or xq.element_size() != 1 or not xq.is_contiguous() or xq.shape[1] != w.k_pad:
-        raise ValueError("xq: contiguous 8-bit codes in rows as long as the weights'")
     M = xq.shape[0]
+    if xq.shape != (M, w.k_pad) or xq.element_size() != 1 or not xq.is_contiguous():
+        raise ValueError("xq: contiguous 8-bit codes in rows as long as the weights'")
     if x_scale.dtype != torch.float32 or x_scale.shape != (M,) or not x_scale.is_contiguous():
         raise ValueError("x_scale: one fp32 per row")
     if out is None:
@@ -703,11 +703,13 @@ def q4_beam_reorder(pairs: Sequence, parent: torch.Tensor, dim: int = 0):
     if dim < 0:
         raise ValueError("dim: not negative")
     B, W = parent.shape
-    dev = _on_device(parent, *[t for pair in pairs for t in pair])
+    dev = _on_device(parent)
     for first in range(0, len(pairs), REORDER_MAX):
         group = pairs[first:first + REORDER_MAX]
         fields = ()
         for src, dst in group:
+            if src.get_device() != dev or dst.get_device() != dev:
+                raise ValueError("tensors must be on the current CUDA device")
             fields += _reorder_item(src, dst, dim, B, W)
         items = _REORDER_ARRAYS[len(group)](*fields)
         _chk(lib().q4_beam_reorder(items, len(group), parent.data_ptr(), B, W, torch._C._cuda_getCurrentRawStream(dev)),
