@@ -63,7 +63,14 @@ template <> struct Vec<float> {
     v[2] = __uint_as_float(r.z);
     v[3] = __uint_as_float(r.w);
   }
+  __device__ static __forceinline__ float top(const uint4& r) {
+    return fmaxf(max3(__uint_as_float(r.x), __uint_as_float(r.y), __uint_as_float(r.z)), __uint_as_float(r.w));
+  }
 };
+template <typename T2> __device__ __forceinline__ T2 max_of_pairs(const uint4& r) {   // (a NaN loses here too)
+  const T2* p = reinterpret_cast<const T2*>(&r);
+  return __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3]));
+}
 template <> struct Vec<__half> {
   static constexpr int N = 8;
   __device__ static __forceinline__ void get(const uint4& r, float (&v)[8]) {
@@ -75,6 +82,10 @@ template <> struct Vec<__half> {
       v[2 * i + 1] = f.y;
     }
   }
+  __device__ static __forceinline__ float top(const uint4& r) {
+    const float2 f = __half22float2(max_of_pairs<__half2>(r));
+    return fmaxf(f.x, f.y);
+  }
 };
 template <> struct Vec<__nv_bfloat16> {
   static constexpr int N = 8;
@@ -85,6 +96,10 @@ template <> struct Vec<__nv_bfloat16> {
       v[2 * i] = __uint_as_float(w[i] << 16);
       v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
     }
+  }
+  __device__ static __forceinline__ float top(const uint4& r) {
+    const float2 f = __bfloat1622float2(max_of_pairs<__nv_bfloat162>(r));
+    return fmaxf(f.x, f.y);
   }
 };
 template <typename T> __device__ __forceinline__ uint4 lowest_vector();
@@ -277,14 +292,7 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
   auto turn = [&](const uint4 (&raw)[ROW_VECTORS], int t) {
     float vector_top[ROW_VECTORS], top = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < ROW_VECTORS; ++j) {
-      float x[N];
-      Vec<T>::get(raw[j], x);
-      vector_top[j] = max3(x[0], x[1], x[2]);
-#pragma unroll
-      for (int i = 3; i + 1 < N; i += 2) vector_top[j] = max3(vector_top[j], x[i], x[i + 1]);
-      vector_top[j] = fmaxf(vector_top[j], x[N - 1]);
-    }
+    for (int j = 0; j < ROW_VECTORS; ++j) vector_top[j] = Vec<T>::top(raw[j]);
 #pragma unroll
     for (int j = 0; j < ROW_VECTORS; j += 2) top = max3(top, vector_top[j], vector_top[j + 1]);
     m = fmaxf(m, top);
