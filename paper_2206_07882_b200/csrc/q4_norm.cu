@@ -239,14 +239,14 @@ __device__ __forceinline__ void pack(Vec<__nv_bfloat16>& v, const float (&f)[8])
 // A row per group of THREADS threads; everything is read and written once, the products v lie in registers, NV vectors of 16 bytes of
 // the row a thread.  WHOLE: rows are 16-byte aligned and a multiple of that long.
 // Long rows are bound by memory (4096 x 4096 with a residual: fp32 36.9 us, 5.9 TB/s; bf16 24.4 us, 4.8 TB/s), short ones of 16 bits
-// by their instructions, about 16 for each element (16000 x 1280 fp16 alone: 20.1 us, 3.1 TB/s).  One warp a row needs no barrier; wider
+// by their instructions, about 15 for each element (16000 x 1280 fp16 alone: 18.0 us, 3.4 TB/s; with a sixth vector that holds nothing 20.6).  One warp a row needs no barrier; wider
 // groups take rows that a warp's registers do not hold, and few rows, where a row's latency is the call's (16 x 1024: 2.2 us).
 // Forming the products again for the codes, for registers of half as many bits, took 10 % more.  Rows that are not 16-byte
 // aligned (4096 x 4001 bf16) take 49 us; element by element they took 75.
-// Threads of a block: four rows of one warp, or one row.  Blocks of an SM: 64 registers a thread for up to 16 elements, 80 for up to 32, 96 and 128 for up to 48 and 64
+// Threads of a block: four rows of one warp, or one row.  Blocks of an SM: 64 registers a thread for up to 16 elements, 80 for up to 40, 96 and 128 for up to 48 and 64
 __host__ __device__ constexpr int norm_threads(int threads) { return threads > 32 ? threads : 128; }
 __host__ __device__ constexpr int norm_blocks(int threads, int elements) {
-  return 128 * (elements <= 16 ? 8 : elements <= 32 ? 6 : elements <= 48 ? 5 : 4) / norm_threads(threads);
+  return 128 * (elements <= 16 ? 8 : elements <= 40 ? 6 : elements <= 48 ? 5 : 4) / norm_threads(threads);
 }
 template <typename T, int THREADS, int NV, bool WHOLE>
 __global__ void __launch_bounds__(norm_threads(THREADS), norm_blocks(THREADS, NV * (16 / (int)sizeof(T)))) k_rmsnorm_quantize(const __grid_constant__ NormArgs a) {
@@ -383,12 +383,30 @@ __global__ void __launch_bounds__(512) k_rmsnorm_quantize_long(const __grid_cons
   }
 }
 
-template <typename T, int THREADS, int NV>
-cudaError_t launch_rows(const NormArgs& a, bool whole, cudaStream_t s) {
+template <typename T, int THREADS, int NV, bool WHOLE>
+cudaError_t launch_rows(const NormArgs& a, cudaStream_t s) {
   constexpr int ROWS = norm_threads(THREADS) / THREADS;
   const long long blocks = (a.rows + ROWS - 1) / ROWS;
-  return launch_ex(whole ? k_rmsnorm_quantize<T, THREADS, NV, true> : k_rmsnorm_quantize<T, THREADS, NV, false>,
-                   dim3((unsigned)(blocks < (1 << 20) ? blocks : 1 << 20)), dim3(norm_threads(THREADS)), 0, s, true, 1, a);
+  return launch_ex(k_rmsnorm_quantize<T, THREADS, NV, WHOLE>, dim3((unsigned)(blocks < (1 << 20) ? blocks : 1 << 20)),
+                   dim3(norm_threads(THREADS)), 0, s, true, 1, a);
+}
+// Vectors of a thread at most: 48 elements of 16 bits, 32 of 32; in the widest group 64 of 16 bits.
+template <typename T> constexpr int MOST = sizeof(T) == 4 ? 8 : 6;
+template <typename T, int THREADS>
+cudaError_t launch_group(const NormArgs& a, int nv, bool whole, cudaStream_t s) {
+  constexpr int ALL = THREADS == 512 ? 8 : MOST<T>;
+  if (whole) switch (nv) {
+    case 1: case 2: return launch_rows<T, THREADS, 2, true>(a, s);
+    case 3: return launch_rows<T, THREADS, 3, true>(a, s);
+    case 4: return launch_rows<T, THREADS, 4, true>(a, s);
+    case 5: return launch_rows<T, THREADS, 5, true>(a, s);
+    case 6: return launch_rows<T, THREADS, 6, true>(a, s);
+    default: return launch_rows<T, THREADS, ALL, true>(a, s);
+  }
+  return nv <= 2   ? launch_rows<T, THREADS, 2, false>(a, s)
+         : nv <= 4 ? launch_rows<T, THREADS, 4, false>(a, s)
+         : nv <= 6 ? launch_rows<T, THREADS, 6, false>(a, s)
+                   : launch_rows<T, THREADS, ALL, false>(a, s);
 }
 template <typename T>
 cudaError_t launch_norm(const NormArgs& a, cudaStream_t s) {
@@ -397,21 +415,21 @@ cudaError_t launch_norm(const NormArgs& a, cudaStream_t s) {
   if (a.rows > 1) low |= (uintptr_t)(a.x_ld | a.r_ld | a.s_ld) * sizeof(T);
   const bool whole = low % 16 == 0;
   const int vectors = a.k_pad / Vec<T>::N;
-  constexpr int MOST = 32 / Vec<T>::N;      // vectors of a thread in wide groups: 32 elements in registers
-  // Many rows: the narrowest group that holds a row (3000 x 2048 fp16: 64 threads 8.0 us, a warp 9.7; 16000 x 1280: 21.9 and 20.1).
-  // Few (less than 16 for each SM): no more than two vectors a thread.
-  if (a.rows >= 16LL * sm_count()) {
-    if (vectors <= 32 * 2) return launch_rows<T, 32, 2>(a, whole, s);
-    if (vectors <= 32 * 4) return launch_rows<T, 32, 4>(a, whole, s);
-    if (vectors <= 32 * 6) return launch_rows<T, 32, 6>(a, whole, s);
-    if (vectors <= 64 * 4) return launch_rows<T, 64, 4>(a, whole, s);
-    if (vectors <= 128 * MOST) return launch_rows<T, 128, MOST>(a, whole, s);
-    if (vectors <= 256 * MOST) return launch_rows<T, 256, MOST>(a, whole, s);
-  }
-  if (vectors <= 128 * 2) return launch_rows<T, 128, 2>(a, whole, s);
-  if (vectors <= 512 * 2) return launch_rows<T, 512, 2>(a, whole, s);
-  if (vectors <= 512 * MOST) return launch_rows<T, 512, MOST>(a, whole, s);
-  if (vectors <= 512 * 8) return launch_rows<T, 512, 8>(a, whole, s);
+  // The narrowest group that holds a row, then wider ones while the rows' threads would not fill the SMs (768 threads are what one holds
+  // of most of these kernels; for narrow groups and 16 bits twice as many).  bf16, us: rows of 4096 with 128 threads of 4 vectors and with 256
+  // of 2, 300 rows 5.2 and 4.9, 1200 rows 7.7 and 8.2, 16000 rows 55 and 71; rows of 1024 with 32 of 4 and 64 of 2, 2048 rows 5.9 and
+  // 4.8, 16000 rows 15.6 and 19.3.
+  const long long fill = 768LL * sm_count();
+  int threads = 32;
+  while (threads < 512 && vectors > threads * MOST<T>) threads *= 2;
+  while (threads < 128 && vectors > threads * 2 && a.rows * threads < fill * (4 / (int)sizeof(T))) threads *= 2;
+  while (threads >= 128 && threads < 512 && vectors > threads * 3 && a.rows * threads < fill) threads *= 2;
+  const int nv = (vectors + threads - 1) / threads;
+  if (threads == 32) return launch_group<T, 32>(a, nv, whole, s);
+  if (threads == 64) return launch_group<T, 64>(a, nv, whole, s);
+  if (threads == 128) return launch_group<T, 128>(a, nv, whole, s);
+  if (threads == 256) return launch_group<T, 256>(a, nv, whole, s);
+  if (nv <= 8) return launch_group<T, 512>(a, nv, whole, s);
   return launch_ex(k_rmsnorm_quantize_long<T>, dim3((unsigned)(a.rows < (1 << 20) ? a.rows : 1 << 20)), dim3(512), 0, s, true, 1, a);
 }
 

@@ -100,6 +100,27 @@ def test_norm_of_many_rows(Bd, dtype, rows, k):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("vectors", [1, 32, 66, 97, 129, 160, 192, 193, 256, 257, 320, 380, 385, 448, 512, 514, 640, 760, 770, 896, 1024, 1026, 1280, 1530, 1538, 1700,
+                                     2048, 2050, 2560, 3070, 3584, 4096])
+def test_norm_of_every_group(Bd, dtype, vectors):
+    # rows of so many 16-byte vectors: few rows, enough for one wave of blocks, and many, so that every number of threads of a row
+    # and of vectors of a thread is met; rows that begin at a multiple of 16 bytes, and one element behind it
+    k = vectors * (4 if dtype == torch.float32 else 8)
+    wave = (1900 if dtype == torch.float32 else 3600) if vectors <= 256 else 1300 if vectors <= 512 else 600
+    for rows in [5] + ([wave, 7300 if vectors <= 320 else 3600 if vectors <= 512 else 1300] if vectors <= 1024 else [600] if vectors <= 2048 else []):
+        g = torch.Generator(device="cuda").manual_seed(rows * 31 + vectors)
+        gain = 1 + 0.2 * torch.randn(k, generator=g, device="cuda")
+        for odd in (0, 1):
+            x, r, out = (torch.randn(rows, k + 8 * odd, generator=g, device="cuda").to(dtype)[:, odd:k + odd] for _ in range(3))
+            for residual in (None, r):
+                codes, scale = Bd.q4_rmsnorm_quantize(x, gain, 1e-5, residual=residual, sum_out=None if residual is None else out)
+                h, want, want_scale = norm_oracle(x, gain, 1e-5, residual)
+                assert torch.equal(codes.view(torch.int8)[:, :k].double(), want)
+                assert ((scale.double() - want_scale).abs() <= SCALE_RTOL * want_scale).all()
+                assert residual is None or torch.equal(out, h)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("k", [64, 1003, 9001])
 def test_norm_of_values_next_to_a_half(Bd, dtype, k):
     # a row maximum of 127 (or 254) makes many quotients exact halves, which go to the even neighbour
