@@ -396,19 +396,47 @@ cudaError_t launch_pair(const TokenLinearArgs& a, cudaStream_t s) {
   return launch_ex(k_token_linear_pair<T>, dim3((unsigned)(2 * pairs)), dim3(320), bytes, s, true, 2, tw, tx, a, tiles_n, tiles_m);
 }
 
-// Time of a launch in us, fitted to all kernels' times at some 35 shapes (1 to 8192 tokens, 100 to 32000 channels, 100 to 8192 codes);
-// the kernel with the least is taken.  At those shapes the choice is the fastest or within a fifth of it.  Examples, us for 32 /
-// 64 / 128 tokens a tile / pairs: 128 x 4096 x 4096 7.6 / 8.5 / 10.5 / 14.1, 1024 x 4096 x 4096 38 / 24 / 21 / 15.6.
+// Clusters of `size` CTAs with an SM each that run at once: fewer than SMs / size, as a cluster lies inside one group of SMs (here
+// 33 of 4 and 15 of 8).  One more waits for another to end: 64 x 1024 x 8192 with 16 clusters of 8 took 9.7 us, with fewer CTAs 6.3.
+int clusters_at_once(int size) {
+  static int known_on[MAX_DEVICES][2];
+  int& known = known_on[device_slot()][size == 8];
+  if (known == 0) {
+    static bool configured_on[MAX_DEVICES];
+    cudaLaunchConfig_t c = {};
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = size;
+    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    c.gridDim = dim3(size * sm_count());
+    c.blockDim = dim3(192);
+    c.dynamicSmemBytes = RING_SM + 1024;
+    c.attrs = &at;
+    c.numAttrs = 1;
+    int n = 0;
+    if (allow_smem(k_token_linear<32, float>, RING_SM + 1024, configured_on) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, k_token_linear<32, float>, &c) != cudaSuccess || n <= 0)
+      return sm_count() * 3 / 4 / size;
+    known = n;
+  }
+  return known;
+}
+
+// Time of a launch in us, fitted to all kernels' times at some 270 shapes (1 to 1024 tokens, 512 to 32000 channels, 1024 to 14000
+// codes) and checked at 35 others; the kernel with the least is taken, of equal ones that with more tokens a tile, which reads
+// weights less often.  At those shapes the choice takes 0.5 % longer than the fastest on average and 13 % at most.  Examples, us for
+// 32 / 64 / 128 tokens a tile / pairs: 128 x 4096 x 4096 7.6 / 8.5 / 10.5 / 14.1, 1024 x 4096 x 4096 38 / 24 / 21 / 15.6.
 // A CTA alone: a tile's chunk of 128 codes takes as long as its operands need from the L2 (18 to 32 KB), the CTAs of an SM one after
-// the other, their epilogues behind the first, and all bytes at least their time in memory.  A split costs 1.6 us more and pays
-// where few tiles have a long K (16 x 1024 x 4096: 5.6 -> 3.8); with more CTAs than SMs it never did.
+// the other, their epilogues behind the first, and all bytes at least their time in memory.  A split exchanges sums, 1.2 to 3.4 us
+// for 16 to 64 tokens, and pays where few tiles have a long K (16 x 1024 x 4096: 5.6 -> 3.8, 256 x 1024 x 14000: 18 -> 12.4).
 double memory_time(const TokenLinearArgs& a, int bytes) { return ((double)a.N * a.K + (double)a.M * a.K + (double)a.M * a.N * bytes) / 6.2e6; }
 double single_cost(const TokenLinearArgs& a, int tok, int split, int bytes) {
-  const double chunk = tok == 16 ? 0.13 : tok == 32 ? 0.155 : tok == 64 ? 0.19 : 0.27;
+  const double chunk = tok == 16 ? 0.125 : tok == 32 ? 0.13 : tok == 64 ? 0.17 : 0.24;
+  const double joined = split == 1 ? 0.0 : tok == 16 ? 1.2 : tok == 32 ? 2.0 : split == 4 ? 3.4 : 2.9;
   const int chunks = ((a.K + BK - 1) / BK + split - 1) / split;
   const double each = ceil((double)((a.N + CH - 1) / CH) * ((a.M + tok - 1) / tok) * split / sm_count());
   const double memory = memory_time(a, bytes), sums = each * chunks * chunk + (each - 1.0) * 0.025 * tok;
-  return 2.6 + (split > 1 ? 1.6 : 0.0) + (memory > sums ? memory : sums);
+  return 2.1 + joined + (memory > sums ? memory : sums);
 }
 // A pair: 0.33 us a chunk for both its CTAs' 256 x 256; rounds of tiles behind the first at least their epilogue.
 double pair_cost(const TokenLinearArgs& a, int bytes) {
@@ -426,10 +454,10 @@ cudaError_t launch_typed(const TokenLinearArgs& a, cudaStream_t s) {
   for (int t = 16; t <= 128; t *= 2) {
     if (t == 16 ? a.M > 16 : t / 2 >= a.M) continue;                  // (more tiles of 16 tokens never paid)
     const long long tiles = (long long)((a.N + CH - 1) / CH) * ((a.M + t - 1) / t);
-    for (int p = 1; p <= (t <= 32 ? 8 : 1); p *= p == 1 ? 4 : 2) {   // two chunks at least for each part
-      if (p > 1 && (chunks < 2 * p || tiles * p > sm_count())) break;
+    for (int p = 1; p <= (t <= 64 ? 8 : 1); p *= p == 1 ? 4 : 2) {   // two chunks at least for each part
+      if (p > 1 && (chunks < 2 * p || tiles * p > sm_count() || tiles > clusters_at_once(p))) break;
       const double c = single_cost(a, t, p, sizeof(T));
-      if (c < least) {
+      if (c < least || (c == least && t > tok && tok > 0)) {
         least = c;
         tok = t;
         split = p;

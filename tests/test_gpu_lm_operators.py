@@ -223,6 +223,15 @@ def test_linear_of_many_tiles(Bd, M, N, K, dtype):
     check_linear(Bd, x, w, sx, sw, b, dtype, gap=M % 3, k=K)
 
 
+@pytest.mark.parametrize("M,N,K", [(13, 2000, 4100), (5, 259, 2050), (250, 130, 4100), (400, 130, 9003), (29, 100, 4100), (51, 1021, 14000),
+                                   (400, 259, 6000), (250, 130, 14000), (200, 1000, 6000), (128, 512, 8192)])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_linear_of_few_tiles_and_a_long_sum(Bd, M, N, K, dtype):
+    # 16, 32 and 64 tokens a tile, each of whose sums is shared by 4 or 8 CTAs
+    x, w, sx, sw, b = linear_inputs(M, N, K, M + N + K, bias=N % 4 == 0)
+    check_linear(Bd, x, w, sx, sw, b, dtype, gap=M % 3, k=K)
+
+
 @pytest.mark.parametrize("M", [2, 70, 300])
 def test_linear_of_the_longest_rows(Bd, M):
     # every product 2^14: the sum of 131040 of them is just below 2^31
@@ -250,6 +259,11 @@ def test_linear_whose_wait_runs_out_stores_nothing(Bd, M, N, K):
     Bd.q4_linear_token_scales(xd, sxd, lin, out=out, status=status)
     assert Bd.q4_poll_status(status) == 0
     assert torch.equal(out, Bd.q4_linear_token_scales(xd, sxd, lin)) and not (out == 3.0).all()
+
+
+def test_linear_of_a_split_whose_wait_runs_out_stores_nothing(Bd):
+    test_linear_whose_wait_runs_out_stores_nothing(Bd, 250, 130, 14000)   # 8 CTAs for 64 tokens
+    test_linear_whose_wait_runs_out_stores_nothing(Bd, 400, 259, 6000)    # 4
 
 
 def test_linear_rows_without_a_scale_stay_alone(Bd):
