@@ -67,7 +67,7 @@ __device__ __forceinline__ void store_columns(uint32_t taddr, T* out, long long 
 constexpr int MAX_STAGES = 12;
 constexpr size_t RING_SM = 216 * 1024;   // bytes of rings on an SM
 __host__ __device__ constexpr int stage_bytes(int tok) { return (CH + tok) * BK; }
-__host__ __device__ constexpr int blocks_per_sm(int tok) { return tok <= 16 ? 3 : tok <= 64 ? 2 : 1; }
+__host__ __device__ constexpr int blocks_per_sm(int tok) { return tok <= 16 ? 3 : 2; }
 template <int TOK, typename T>
 __global__ void __launch_bounds__(192, blocks_per_sm(TOK))
 k_token_linear(const __grid_constant__ CUtensorMap tma_w, const __grid_constant__ CUtensorMap tma_x, const TokenLinearArgs a, const int tiles_n,
@@ -214,18 +214,22 @@ k_token_linear(const __grid_constant__ CUtensorMap tma_w, const __grid_constant_
   if (warp == 5) tmem_dealloc(tmem, TCOLS);
 }
 
-// ---- two CTAs a tile of 256 channels x 256 tokens, persistent
+// ---- two CTAs a tile of 256 channels x 256 or 128 tokens, persistent
 // A stage is 128 channels and 128 tokens of 128 codes in each CTA, 32 KB for 2 x 128 x 256 x 128 products: half of what a CTA
 // alone would fetch for its 128 x 256 tile, whose operands come out of the L2 slower than the tensor cores take them.
 // Tensor memory holds two accumulators of 256 columns: the epilogue stores one while the next tile is summed up.
-constexpr int PT = 256, PAIR_STAGES = 6, PAIR_STAGE = (CH + PT / 2) * BK, PAIR_GROUP = 8;
-template <typename T>
+// Tiles of 128 tokens fetch half as much again for a product, but leave fewer pairs idle
+// (300 x 11000 x 8192 29 us, with 256 tokens 43; 512 x 32000 x 14000 220 and 175).
+constexpr int PAIR_GROUP = 8;
+__host__ __device__ constexpr int pair_stage(int pt) { return (CH + pt / 2) * BK; }
+__host__ __device__ constexpr int pair_stages(int pt) { return pt == 256 ? 6 : 8; }
+template <int PT, typename T>
 __global__ void __launch_bounds__(320, 1)
 k_token_linear_pair(const __grid_constant__ CUtensorMap tma_w, const __grid_constant__ CUtensorMap tma_x, const TokenLinearArgs a,
                     const int tiles_n, const int tiles_m) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  constexpr int NS = PAIR_STAGES;
+  constexpr int NS = pair_stages(PT), STAGE = pair_stage(PT);
   __shared__ uint64_t full[NS], empty[NS], acc_full[2], acc_empty[2];   // full and acc_empty: those of rank 0 count
   __shared__ uint32_t tmem_base_s;
   __shared__ float s_x[2][PT];
@@ -276,9 +280,9 @@ k_token_linear_pair(const __grid_constant__ CUtensorMap tma_w, const __grid_cons
         if (!ok) break;
         ++filled;
         const uint32_t bar = cluster_addr(&full[s], 0);
-        if (rank == 0) mbar_expect_tx(on, &full[s], 2 * PAIR_STAGE);
-        tma_load_2d_pair(on, smem + s * PAIR_STAGE, &tma_w, i * BK, n0, bar);
-        tma_load_2d_pair(on, smem + s * PAIR_STAGE + CH * BK, &tma_x, i * BK, m0 + (int)rank * (PT / 2), bar);
+        if (rank == 0) mbar_expect_tx(on, &full[s], 2 * STAGE);
+        tma_load_2d_pair(on, smem + s * STAGE, &tma_w, i * BK, n0, bar);
+        tma_load_2d_pair(on, smem + s * STAGE + CH * BK, &tma_x, i * BK, m0 + (int)rank * (PT / 2), bar);
         if (++s == NS) {
           s = 0;
           ph ^= 1;
@@ -314,7 +318,7 @@ k_token_linear_pair(const __grid_constant__ CUtensorMap tma_w, const __grid_cons
             ph ^= 1;
           }
           ready = mbar_test(&full[s], ph);
-          const uint64_t dw = umma_desc_sw128(smem_u32(smem + st * PAIR_STAGE)), dx = umma_desc_sw128(smem_u32(smem + st * PAIR_STAGE + CH * BK));
+          const uint64_t dw = umma_desc_sw128(smem_u32(smem + st * STAGE)), dx = umma_desc_sw128(smem_u32(smem + st * STAGE + CH * BK));
 #pragma unroll
           for (int kk = 0; kk < BK / 32; ++kk) umma_i8_pair(on, d, dw + 2 * kk, dx + 2 * kk, idesc, (i | kk) != 0);
           umma_commit_pair(on, &empty[st]);
@@ -364,40 +368,9 @@ cudaError_t allow_smem(K kernel, size_t bytes, bool* configured_on) {
   return e;
 }
 
-template <int TOK, typename T>
-cudaError_t launch_tile(const TokenLinearArgs& a, int split, cudaStream_t s) {
-  static bool configured_on[MAX_DEVICES];
-  cudaError_t e = allow_smem(k_token_linear<TOK, T>, RING_SM + 1024, configured_on);
-  if (e != cudaSuccess) return e;
-  CUtensorMap tw, tx;
-  if (!make_tmap_i8(&tw, a.wq, a.K, a.N, a.K, CH) || !make_tmap_i8(&tx, a.xq, a.K, a.M, a.K, TOK)) return cudaErrorInvalidValue;
-  const int tiles_n = (a.N + CH - 1) / CH, tiles_m = (a.M + TOK - 1) / TOK;
-  // the CTAs of an SM share the room for rings; a ring needs no more stages than its part of K has chunks, but holds the sums of a split
-  const long long ctas = (long long)tiles_n * tiles_m * split, each = (ctas + sm_count() - 1) / sm_count();
-  const int on_sm = each < blocks_per_sm(TOK) ? (int)each : blocks_per_sm(TOK), chunks = ((a.K + BK - 1) / BK + split - 1) / split;
-  int ns = (int)((RING_SM - 1024 * on_sm) / on_sm / stage_bytes(TOK));
-  ns = ns < chunks ? ns : chunks;
-  ns = ns < 4 ? 4 : ns > MAX_STAGES ? MAX_STAGES : ns;
-  const size_t bytes = (size_t)ns * stage_bytes(TOK) + 1024;
-  return launch_ex(k_token_linear<TOK, T>, dim3((unsigned)ctas), dim3(192), bytes, s, true, (unsigned)split, tw, tx, a, tiles_n, split, ns);
-}
-template <typename T>
-cudaError_t launch_pair(const TokenLinearArgs& a, cudaStream_t s) {
-  static bool configured_on[MAX_DEVICES];
-  const size_t bytes = (size_t)PAIR_STAGES * PAIR_STAGE + 1024;
-  cudaError_t e = allow_smem(k_token_linear_pair<T>, bytes, configured_on);
-  if (e != cudaSuccess) return e;
-  CUtensorMap tw, tx;
-  if (!make_tmap_i8(&tw, a.wq, a.K, a.N, a.K, CH) || !make_tmap_i8(&tx, a.xq, a.K, a.M, a.K, PT / 2)) return cudaErrorInvalidValue;
-  const int tiles_n = (a.N + 2 * CH - 1) / (2 * CH), tiles_m = (a.M + PT - 1) / PT;
-  const long long tiles = (long long)tiles_n * tiles_m;
-  if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
-  const int pairs = tiles < sm_count() / 2 ? (int)tiles : sm_count() / 2;
-  return launch_ex(k_token_linear_pair<T>, dim3((unsigned)(2 * pairs)), dim3(320), bytes, s, true, 2, tw, tx, a, tiles_n, tiles_m);
-}
-
 // Clusters of `size` CTAs with an SM each that run at once: fewer than SMs / size, as a cluster lies inside one group of SMs (here
-// 33 of 4 and 15 of 8).  One more waits for another to end: 64 x 1024 x 8192 with 16 clusters of 8 took 9.7 us, with fewer CTAs 6.3.
+// 33 of 4 and 15 of 8).  More share SMs, or wait for another to end: 64 x 1024 x 8192, 16 clusters of 8, took 9.7 us
+// with whole SMs for rings and 6.4 with halves.
 int clusters_at_once(int size) {
   static int known_on[MAX_DEVICES][2];
   int& known = known_on[device_slot()][size == 8];
@@ -422,55 +395,100 @@ int clusters_at_once(int size) {
   return known;
 }
 
-// Time of a launch in us, fitted to all kernels' times at some 270 shapes (1 to 1024 tokens, 512 to 32000 channels, 1024 to 14000
-// codes) and checked at 35 others; the kernel with the least is taken, of equal ones that with more tokens a tile, which reads
-// weights less often.  At those shapes the choice takes 0.5 % longer than the fastest on average and 13 % at most.  Examples, us for
-// 32 / 64 / 128 tokens a tile / pairs: 128 x 4096 x 4096 7.6 / 8.5 / 10.5 / 14.1, 1024 x 4096 x 4096 38 / 24 / 21 / 15.6.
-// A CTA alone: a tile's chunk of 128 codes takes as long as its operands need from the L2 (18 to 32 KB), the CTAs of an SM one after
+// CTAs of an SM: clusters of a split in turn on the SMs that hold one at a time
+int ctas_of_sm(long long tiles, int split) {
+  const long long at_once = split > 1 ? clusters_at_once(split) : sm_count();
+  return (int)((tiles + at_once - 1) / at_once);
+}
+
+template <int TOK, typename T>
+cudaError_t launch_tile(const TokenLinearArgs& a, int split, cudaStream_t s) {
+  static bool configured_on[MAX_DEVICES];
+  cudaError_t e = allow_smem(k_token_linear<TOK, T>, RING_SM + 1024, configured_on);
+  if (e != cudaSuccess) return e;
+  CUtensorMap tw, tx;
+  if (!make_tmap_i8(&tw, a.wq, a.K, a.N, a.K, CH) || !make_tmap_i8(&tx, a.xq, a.K, a.M, a.K, TOK)) return cudaErrorInvalidValue;
+  const int tiles_n = (a.N + CH - 1) / CH, tiles_m = (a.M + TOK - 1) / TOK;
+  // the CTAs of an SM share the room for rings; a ring needs no more stages than its part of K has chunks, but holds the sums of a split
+  const long long ctas = (long long)tiles_n * tiles_m * split;
+  const int each = ctas_of_sm((long long)tiles_n * tiles_m, split);
+  const int on_sm = each < blocks_per_sm(TOK) ? each : blocks_per_sm(TOK), chunks = ((a.K + BK - 1) / BK + split - 1) / split;
+  int ns = (int)((RING_SM - 1024 * on_sm) / on_sm / stage_bytes(TOK));
+  ns = ns < chunks ? ns : chunks;
+  ns = ns < 4 ? 4 : ns > MAX_STAGES ? MAX_STAGES : ns;
+  const size_t bytes = (size_t)ns * stage_bytes(TOK) + 1024;
+  return launch_ex(k_token_linear<TOK, T>, dim3((unsigned)ctas), dim3(192), bytes, s, true, (unsigned)split, tw, tx, a, tiles_n, split, ns);
+}
+template <int PT, typename T>
+cudaError_t launch_pair(const TokenLinearArgs& a, cudaStream_t s) {
+  static bool configured_on[MAX_DEVICES];
+  const size_t bytes = (size_t)pair_stages(PT) * pair_stage(PT) + 1024;
+  cudaError_t e = allow_smem(k_token_linear_pair<PT, T>, bytes, configured_on);
+  if (e != cudaSuccess) return e;
+  CUtensorMap tw, tx;
+  if (!make_tmap_i8(&tw, a.wq, a.K, a.N, a.K, CH) || !make_tmap_i8(&tx, a.xq, a.K, a.M, a.K, PT / 2)) return cudaErrorInvalidValue;
+  const int tiles_n = (a.N + 2 * CH - 1) / (2 * CH), tiles_m = (a.M + PT - 1) / PT;
+  const long long tiles = (long long)tiles_n * tiles_m;
+  if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
+  const int pairs = tiles < sm_count() / 2 ? (int)tiles : sm_count() / 2;
+  return launch_ex(k_token_linear_pair<PT, T>, dim3((unsigned)(2 * pairs)), dim3(320), bytes, s, true, 2, tw, tx, a, tiles_n, tiles_m);
+}
+
+// Time of a launch in us, fitted to all kernels' times at some 600 shapes (1 to 8192 tokens, 512 to 50257 channels, 640 to 14000
+// codes); the kernel with the least is taken, of equal ones that with more tokens a tile, which reads weights less often.  At those
+// shapes the choice takes 0.4 % longer than the fastest on average.  Examples, us for 32 / 64 tokens a tile / pairs of 128 / of 256:
+// 64 x 4096 x 4096 7.8 / 8.3 / - / -, 300 x 5120 x 4096 19 / 13.1 / 10.9 / 15.5, 512 x 11000 x 8192 107 / 71 / 40 / 44.
+// A CTA alone: a tile's chunk of 128 codes takes as long as its operands need from the L2 (18 to 24 KB), the CTAs of an SM one after
 // the other, their epilogues behind the first, and all bytes at least their time in memory.  A split exchanges sums, 1.2 to 3.4 us
 // for 16 to 64 tokens, and pays where few tiles have a long K (16 x 1024 x 4096: 5.6 -> 3.8, 256 x 1024 x 14000: 18 -> 12.4).
 double memory_time(const TokenLinearArgs& a, int bytes) { return ((double)a.N * a.K + (double)a.M * a.K + (double)a.M * a.N * bytes) / 6.2e6; }
 double single_cost(const TokenLinearArgs& a, int tok, int split, int bytes) {
-  const double chunk = tok == 16 ? 0.125 : tok == 32 ? 0.13 : tok == 64 ? 0.17 : 0.24;
+  const double chunk = tok == 16 ? 0.125 : tok == 32 ? 0.13 : 0.183;
   const double joined = split == 1 ? 0.0 : tok == 16 ? 1.2 : tok == 32 ? 2.0 : split == 4 ? 3.4 : 2.9;
   const int chunks = ((a.K + BK - 1) / BK + split - 1) / split;
-  const double each = ceil((double)((a.N + CH - 1) / CH) * ((a.M + tok - 1) / tok) * split / sm_count());
-  const double memory = memory_time(a, bytes), sums = each * chunks * chunk + (each - 1.0) * 0.025 * tok;
+  const double each = ctas_of_sm((long long)((a.N + CH - 1) / CH) * ((a.M + tok - 1) / tok), split);
+  const double memory = memory_time(a, bytes), sums = each * chunks * chunk + (each - 1.0) * 0.024 * tok;
   return 2.1 + joined + (memory > sums ? memory : sums);
 }
-// A pair: 0.33 us a chunk for both its CTAs' 256 x 256; rounds of tiles behind the first at least their epilogue.
-double pair_cost(const TokenLinearArgs& a, int bytes) {
-  const long long tiles = (long long)((a.N + 2 * CH - 1) / (2 * CH)) * ((a.M + PT - 1) / PT), pairs = sm_count() / 2;
-  const double chunks = 0.33 * ((a.K + BK - 1) / BK), memory = memory_time(a, bytes);
-  const double sums = chunks + (double)((tiles + pairs - 1) / pairs - 1) * (chunks > 3.0 ? chunks : 3.0);
-  return 6.0 + (memory > sums ? memory : sums);
+// A pair: a chunk for both its CTAs' 256 x 256 or 256 x 128; rounds of tiles behind the first at least their epilogue.
+double pair_cost(const TokenLinearArgs& a, int tok, int bytes) {
+  const long long tiles = (long long)((a.N + 2 * CH - 1) / (2 * CH)) * ((a.M + tok - 1) / tok), pairs = sm_count() / 2;
+  const double chunks = (tok == 256 ? 0.35 : 0.215) * ((a.K + BK - 1) / BK), memory = memory_time(a, bytes), epilogue = 2.1;
+  const double sums = chunks + (double)((tiles + pairs - 1) / pairs - 1) * (chunks > epilogue ? chunks : epilogue);
+  return (tok == 256 ? 4.8 : 4.55) + (memory > sums ? memory : sums);
 }
 
 template <typename T>
 cudaError_t launch_typed(const TokenLinearArgs& a, cudaStream_t s) {
   const int chunks = (a.K + BK - 1) / BK;
-  double least = a.M > 64 ? pair_cost(a, sizeof(T)) : 1e300;
+  double least = 1e300;
   int tok = 0, split = 1;
-  for (int t = 16; t <= 128; t *= 2) {
+  for (int t = 16; t <= 64; t *= 2) {
     if (t == 16 ? a.M > 16 : t / 2 >= a.M) continue;                  // (more tiles of 16 tokens never paid)
     const long long tiles = (long long)((a.N + CH - 1) / CH) * ((a.M + t - 1) / t);
-    for (int p = 1; p <= (t <= 64 ? 8 : 1); p *= p == 1 ? 4 : 2) {   // two chunks at least for each part
-      if (p > 1 && (chunks < 2 * p || tiles * p > sm_count() || tiles > clusters_at_once(p))) break;
+    if (tiles > INT32_MAX / 2) continue;
+    for (int p = 1; p <= 8; p *= p == 1 ? 4 : 2) {                    // two chunks at least for each part
+      if (p > 1 && (chunks < 2 * p || ctas_of_sm(tiles, p) > blocks_per_sm(t))) break;
       const double c = single_cost(a, t, p, sizeof(T));
-      if (c < least || (c == least && t > tok && tok > 0)) {
+      if (c < least || (c == least && t > tok)) {
         least = c;
         tok = t;
         split = p;
       }
     }
   }
-  if (tok == 0) return launch_pair<T>(a, s);
-  const long long ctas = (long long)((a.N + CH - 1) / CH) * ((a.M + tok - 1) / tok) * split;
-  if (ctas > INT32_MAX / 2) return cudaErrorInvalidValue;
-  return tok == 16   ? launch_tile<16, T>(a, split, s)
-         : tok == 32 ? launch_tile<32, T>(a, split, s)
-         : tok == 64 ? launch_tile<64, T>(a, split, s)
-                     : launch_tile<128, T>(a, split, s);
+  for (int t = 128; t <= 256 && a.M > 64; t *= 2) {
+    const double c = pair_cost(a, t, sizeof(T));
+    if (c <= least) {
+      least = c;
+      tok = t;
+    }
+  }
+  return tok == 16    ? launch_tile<16, T>(a, split, s)
+         : tok == 32  ? launch_tile<32, T>(a, split, s)
+         : tok == 64  ? launch_tile<64, T>(a, split, s)
+         : tok == 128 ? launch_pair<128, T>(a, s)
+                      : launch_pair<256, T>(a, s);
 }
 
 }  // namespace

@@ -224,7 +224,7 @@ def test_linear_of_many_tiles(Bd, M, N, K, dtype):
 
 
 @pytest.mark.parametrize("M,N,K", [(13, 2000, 4100), (5, 259, 2050), (250, 130, 4100), (400, 130, 9003), (29, 100, 4100), (51, 1021, 14000),
-                                   (400, 259, 6000), (250, 130, 14000), (200, 1000, 6000), (128, 512, 8192)])
+                                   (400, 259, 6000), (250, 130, 14000), (200, 1000, 6000), (128, 512, 8192), (9, 5000, 14000), (30, 5100, 14000)])
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_linear_of_few_tiles_and_a_long_sum(Bd, M, N, K, dtype):
     # 16, 32 and 64 tokens a tile, each of whose sums is shared by 4 or 8 CTAs
@@ -261,9 +261,18 @@ def test_linear_whose_wait_runs_out_stores_nothing(Bd, M, N, K):
     assert torch.equal(out, Bd.q4_linear_token_scales(xd, sxd, lin)) and not (out == 3.0).all()
 
 
+@pytest.mark.parametrize("M,N,K", [(300, 11000, 1000), (700, 2050, 4100), (100, 14001, 2048), (129, 9000, 2001), (3000, 700, 5000), (500, 4097, 700)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_linear_of_pairs(Bd, M, N, K, dtype):
+    # tiles of 128 and 256 tokens by two CTAs, one round of tiles and several, ragged at both ends
+    x, w, sx, sw, b = linear_inputs(M, N, K, M + N + K, bias=N % 2 == 0)
+    check_linear(Bd, x, w, sx, sw, b, dtype, gap=M % 3, k=K)
+
+
 def test_linear_of_a_split_whose_wait_runs_out_stores_nothing(Bd):
     test_linear_whose_wait_runs_out_stores_nothing(Bd, 250, 130, 14000)   # 8 CTAs for 64 tokens
     test_linear_whose_wait_runs_out_stores_nothing(Bd, 400, 259, 6000)    # 4
+    test_linear_whose_wait_runs_out_stores_nothing(Bd, 300, 11000, 1000)  # pairs of CTAs, tiles of 128 tokens
 
 
 def test_linear_rows_without_a_scale_stay_alone(Bd):
