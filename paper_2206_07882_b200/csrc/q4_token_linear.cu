@@ -45,10 +45,19 @@ __device__ __forceinline__ void store_columns(uint32_t taddr, T* out, long long 
     else
       drained();
     if (c0 + STEP <= tokens) {
+      float4 sc[STEP / 4];
 #pragma unroll
-      for (int i = 0; i < STEP; ++i) {
-        *out = from_f32<T>(__fmaf_rn((float)r[set][i], __fmul_rn(scale[c0 + i], sw), b));
+      for (int i = 0; i < STEP / 4; ++i) sc[i] = *reinterpret_cast<const float4*>(scale + c0 + 4 * i);
+      auto store = [&](int v, float s) {
+        *out = from_f32<T>(__fmaf_rn((float)v, __fmul_rn(s, sw), b));
         out += ldo;
+      };
+#pragma unroll
+      for (int i = 0; i < STEP / 4; ++i) {
+        store(r[set][4 * i], sc[i].x);
+        store(r[set][4 * i + 1], sc[i].y);
+        store(r[set][4 * i + 2], sc[i].z);
+        store(r[set][4 * i + 3], sc[i].w);
       }
     } else if (c0 < tokens) {
 #pragma unroll
@@ -74,12 +83,12 @@ k_token_linear(const __grid_constant__ CUtensorMap tma_w, const __grid_constant_
                const int split, const int NS) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  int32_t* part = reinterpret_cast<int32_t*>(smem);   // [split][TOK / split][CH], the sums of all CTAs of a split
+  int32_t* part = reinterpret_cast<int32_t*>(smem);   // [split][TOK / split / 4][CH][4] (or 2 for 4), the sums of all CTAs of a split
   constexpr int W_BYTES = CH * BK, STAGE = W_BYTES + TOK * BK;
   constexpr uint32_t TCOLS = TOK < 32 ? 32 : TOK;
   __shared__ uint64_t full[MAX_STAGES], empty[MAX_STAGES], acc_full;
   __shared__ uint32_t tmem_base_s, failed;
-  __shared__ float s_x[TOK];
+  __shared__ __align__(16) float s_x[TOK];
   const int tid = threadIdx.x, warp = uniform_warp(), lane = tid & 31;
   const int rank = blockIdx.x % split, tile = blockIdx.x / split;
   const int n0 = tile % tiles_n * CH, m0 = tile / tiles_n * TOK, all = (a.K + BK - 1) / BK;
@@ -170,20 +179,21 @@ k_token_linear(const __grid_constant__ CUtensorMap tma_w, const __grid_constant_
     const int log_each = 31 - __clz(TOK / split);
     cluster_arrive();
     cluster_wait();                  // every CTA's products are done (or given up, with its copies landed): its ring may be written to
+    const int each = TOK / split;    // tokens that a CTA finishes
+    const uint32_t to = smem_u32(part) + (uint32_t)(rank * each * CH) * 4;
     if (warp < 4) {
-      const int each = TOK / split;  // tokens that a CTA finishes
-      const uint32_t to = smem_u32(part) + (uint32_t)((rank * each) * CH + ch) * 4;
-      for (int c0 = 0; c0 < TOK; c0 += 8) {
-        int r[8];
+#pragma unroll
+      for (int c0 = 0; c0 < TOK; c0 += 16) {
+        int r[16];
         tmem_ld(tmem + ((uint32_t)(warp * 32) << 16) + c0, r);
         tmem_ld_wait();
+        if (each >= 4) {
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) {   // (each is 2 at least)
-          const int dst = (c0 + i) >> log_each;
-          uint32_t addr;
-          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"(to + (uint32_t)(((c0 + i) & (each - 1)) * CH) * 4), "r"(dst));
-          st_cluster(addr, r[i]);
-          st_cluster(addr + CH * 4, r[i + 1]);
+          for (int i = 0; i < 16; i += 4)
+            st_cluster(cluster_addr_of(to + (uint32_t)(((c0 + i) & (each - 1)) * CH + 4 * ch) * 4, (c0 + i) >> log_each), r[i], r[i + 1], r[i + 2], r[i + 3]);
+        } else {                     // each is 2
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) st_cluster(cluster_addr_of(to + (uint32_t)(2 * ch) * 4, (c0 + i) >> 1), r[i], r[i + 1]);
         }
       }
       if (!ok)                       // nobody stores anything of this tile
@@ -193,14 +203,40 @@ k_token_linear(const __grid_constant__ CUtensorMap tma_w, const __grid_constant_
     cluster_arrive();
     cluster_wait();
     if (warp < 4 && n < a.N && *reinterpret_cast<volatile uint32_t*>(&failed) == 0) {
-      const int each = TOK / split, first = rank * each;
+      const int first = rank * each;
       const float sw = __ldg(a.w_scale + n), b = a.bias ? __ldg(a.bias + n) : 0.0f;
-      T* out = static_cast<T*>(a.out) + n;
-      for (int c = 0; c < each; ++c) {
-        int sum = 0;
-        for (int p = 0; p < split; ++p) sum += part[(p * each + c) * CH + ch];
-        const int m = m0 + first + c;
-        if (m < a.M) out[(long long)m * a.ldo] = from_f32<T>(__fmaf_rn((float)sum, __fmul_rn(s_x[first + c], sw), b));
+      T* out = static_cast<T*>(a.out) + (long long)(m0 + first) * a.ldo + n;
+      auto finish = [&](int c, int sum, float sx) {
+        if (m0 + first + c < a.M) out[(long long)c * a.ldo] = from_f32<T>(__fmaf_rn((float)sum, __fmul_rn(sx, sw), b));
+      };
+      if (each >= 4) {
+#pragma unroll 2
+        for (int c = 0; c < each; c += 4) {
+          int4 sum = make_int4(0, 0, 0, 0);
+#pragma unroll 4
+          for (int p = 0; p < split; ++p) {
+            const int4 v = *reinterpret_cast<const int4*>(part + (p * each + c) * CH + 4 * ch);
+            sum.x += v.x;
+            sum.y += v.y;
+            sum.z += v.z;
+            sum.w += v.w;
+          }
+          const float4 sx = *reinterpret_cast<const float4*>(s_x + first + c);
+          finish(c, sum.x, sx.x);
+          finish(c + 1, sum.y, sx.y);
+          finish(c + 2, sum.z, sx.z);
+          finish(c + 3, sum.w, sx.w);
+        }
+      } else {
+        int2 sum = make_int2(0, 0);
+#pragma unroll 8
+        for (int p = 0; p < split; ++p) {
+          const int2 v = *reinterpret_cast<const int2*>(part + p * 2 * CH + 2 * ch);
+          sum.x += v.x;
+          sum.y += v.y;
+        }
+        finish(0, sum.x, s_x[first]);
+        finish(1, sum.y, s_x[first + 1]);
       }
     }
   } else if (warp < 4) {
@@ -232,7 +268,7 @@ k_token_linear_pair(const __grid_constant__ CUtensorMap tma_w, const __grid_cons
   constexpr int NS = pair_stages(PT), STAGE = pair_stage(PT);
   __shared__ uint64_t full[NS], empty[NS], acc_full[2], acc_empty[2];   // full and acc_empty: those of rank 0 count
   __shared__ uint32_t tmem_base_s;
-  __shared__ float s_x[2][PT];
+  __shared__ __align__(16) float s_x[2][PT];
   const int tid = threadIdx.x, warp = uniform_warp(), lane = tid & 31;
   const uint32_t rank = pair_rank();
   const int pairs = gridDim.x / 2, n_tiles = tiles_n * tiles_m, nk = (a.K + BK - 1) / BK;
@@ -439,12 +475,13 @@ cudaError_t launch_pair(const TokenLinearArgs& a, cudaStream_t s) {
 // shapes the choice takes 0.4 % longer than the fastest on average.  Examples, us for 32 / 64 tokens a tile / pairs of 128 / of 256:
 // 64 x 4096 x 4096 7.8 / 8.3 / - / -, 300 x 5120 x 4096 19 / 13.1 / 10.9 / 15.5, 512 x 11000 x 8192 107 / 71 / 40 / 44.
 // A CTA alone: a tile's chunk of 128 codes takes as long as its operands need from the L2 (18 to 24 KB), the CTAs of an SM one after
-// the other, their epilogues behind the first, and all bytes at least their time in memory.  A split exchanges sums, 1.2 to 3.4 us
-// for 16 to 64 tokens, and pays where few tiles have a long K (16 x 1024 x 4096: 5.6 -> 3.8, 256 x 1024 x 14000: 18 -> 12.4).
+// the other, their epilogues behind the first, and all bytes at least their time in memory.  A split exchanges sums, 1 to 2.2 us
+// for 16 to 64 tokens (16 bytes a store; single words took 1.2 to 3.4), and pays where few tiles have a long K (16 x 1024 x 4096:
+// 5.6 -> 3.6, 256 x 1024 x 14000: 18 -> 10.9).
 double memory_time(const TokenLinearArgs& a, int bytes) { return ((double)a.N * a.K + (double)a.M * a.K + (double)a.M * a.N * bytes) / 6.2e6; }
 double single_cost(const TokenLinearArgs& a, int tok, int split, int bytes) {
   const double chunk = tok == 16 ? 0.125 : tok == 32 ? 0.13 : 0.183;
-  const double joined = split == 1 ? 0.0 : tok == 16 ? 1.2 : tok == 32 ? 2.0 : split == 4 ? 3.4 : 2.9;
+  const double joined = split == 1 ? 0.0 : tok == 16 ? 1.0 : tok == 32 ? 1.5 : 2.2;
   const int chunks = ((a.K + BK - 1) / BK + split - 1) / split;
   const double each = ctas_of_sm((long long)((a.N + CH - 1) / CH) * ((a.M + tok - 1) / tok), split);
   const double memory = memory_time(a, bytes), sums = each * chunks * chunk + (each - 1.0) * 0.024 * tok;
