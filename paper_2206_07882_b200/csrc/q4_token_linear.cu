@@ -424,8 +424,10 @@ int clusters_at_once(int size) {
     c.numAttrs = 1;
     int n = 0;
     if (allow_smem(k_token_linear<32, float>, RING_SM + 1024, configured_on) != cudaSuccess ||
-        cudaOccupancyMaxActiveClusters(&n, k_token_linear<32, float>, &c) != cudaSuccess || n <= 0)
+        cudaOccupancyMaxActiveClusters(&n, k_token_linear<32, float>, &c) != cudaSuccess || n <= 0) {
+      (void)cudaGetLastError();      // (a guess does as well)
       return sm_count() * 3 / 4 / size;
+    }
     known = n;
   }
   return known;

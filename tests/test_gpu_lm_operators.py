@@ -2,6 +2,9 @@
 codes, linear layer with token scales, beam selection over a vocabulary, reordering of states."""
 import ctypes as C
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -665,6 +668,45 @@ def test_rows_further_apart_than_32_bits_count(Bd):
     src, dst = far_rows(rows, step).as_strided((1, 4, 50), (4 * step, step, 1)), torch.zeros(1, 4, 50, dtype=torch.float16, device="cuda")
     Bd.q4_beam_reorder([(src, dst)], torch.tensor([[3, 2, -1, 0]], dtype=torch.int32, device="cuda"))
     assert torch.equal(dst[0].cpu(), torch.stack([rows[3], rows[2], 0 * rows[0], rows[0]]))
+
+
+FIRST_CALLS = """
+import torch
+from paper_2206_07882_b200 import binding as Bd
+torch.manual_seed(1)
+x, gain = torch.randn(64, 8192, device="cuda"), torch.ones(8192, device="cuda")
+wide = torch.randn(2000, 12288, device="cuda")            # (wide groups)
+w = torch.randint(-127, 128, (1024, 8192), device="cuda").to(torch.int8).view(torch.uint8)
+lin = Bd.DeviceLinear.from_mat(Bd.DeviceMat(w, torch.full((1024,), 1e-3, device="cuda"), 1024, 8192, 8192, 8))
+score, cells = torch.randn(4, 16, device="cuda"), torch.randn(4, 16, 100, device="cuda")
+moved = torch.zeros_like(cells)
+torch.cuda.synchronize()
+
+def step():
+    q, s = Bd.q4_rmsnorm_quantize(x, gain, 1e-5)
+    logits = Bd.q4_linear_token_scales(q, s, lin)
+    best = Bd.q4_lm_beam_select(logits.view(4, 16, 1024), score, eos=0)
+    Bd.q4_beam_reorder([(cells, moved)], best["parent"])
+    return [q, s, logits, best["parent"], best["token"], best["score"], *Bd.q4_rmsnorm_quantize(wide, gain.new_ones(12288), 1e-5)]
+
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    got = step()
+graph.replay()
+graph.replay()
+torch.cuda.synchronize()
+kept = moved.clone()
+want = step()
+assert all(torch.equal(g, h) for g, h in zip(got, want)) and torch.equal(kept, moved)
+print("same")
+"""
+
+
+def test_first_calls_of_a_process_are_captured(Bd):
+    # what a first call asks the device or sets up does not disturb a capture
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS], capture_output=True, text=True, timeout=300,
+                       cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert r.returncode == 0 and r.stdout.split() == ["same"], r.stderr[-2000:]
 
 
 # -------------------------------------------------------------------------------------------------------- refusals
