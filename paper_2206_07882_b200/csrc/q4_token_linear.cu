@@ -17,7 +17,7 @@ namespace q4 {
 namespace {
 
 constexpr int BK = 128;        // codes per row of an operand tile
-constexpr int CH = 128;        // output channels of a CTA's tile
+constexpr int CH = 128;        // output channels of a CTA's tile, of most
 
 template <typename T> __device__ __forceinline__ T from_f32(float v);
 template <> __device__ __forceinline__ float from_f32(float v) { return v; }
@@ -70,28 +70,29 @@ __device__ __forceinline__ void store_columns(uint32_t taddr, T* out, long long 
 }
 
 // ---- one CTA a tile; up to 8 CTAs of a cluster share a tile's K
+// Tiles of 64 channels are for SMs that tiles of 128 would leave idle (32 x 4096 x 4096 7.1 -> 6.2 us, 16 x 5120 x 4096 7.5 -> 6.9).
 // What few tokens need is operand bytes in flight, as their weights come from memory once: up to 216 KB in the CTAs of an SM.
 // The CTAs of a split exchange their int32 sums through distributed shared memory (in place of the rings, once all of them are
 // through), each finishing a part of the tokens, so a split changes no result.
-constexpr int MAX_STAGES = 12;
+constexpr int MAX_STAGES = 21;
 constexpr size_t RING_SM = 216 * 1024;   // bytes of rings on an SM
-__host__ __device__ constexpr int stage_bytes(int tok) { return (CH + tok) * BK; }
+__host__ __device__ constexpr int stage_bytes(int tok, int chn) { return (chn + tok) * BK; }
 __host__ __device__ constexpr int blocks_per_sm(int tok) { return tok <= 16 ? 3 : 2; }
-template <int TOK, typename T>
+template <int TOK, int CHN, typename T>
 __global__ void __launch_bounds__(192, blocks_per_sm(TOK))
 k_token_linear(const __grid_constant__ CUtensorMap tma_w, const __grid_constant__ CUtensorMap tma_x, const TokenLinearArgs a, const int tiles_n,
                const int split, const int NS) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  int32_t* part = reinterpret_cast<int32_t*>(smem);   // [split][TOK / split / 4][CH][4] (or 2 for 4), the sums of all CTAs of a split
-  constexpr int W_BYTES = CH * BK, STAGE = W_BYTES + TOK * BK;
+  int32_t* part = reinterpret_cast<int32_t*>(smem);   // [split][TOK / split / 4][CHN][4] (or 2 for 4), the sums of all CTAs of a split
+  constexpr int W_BYTES = CHN * BK, STAGE = W_BYTES + TOK * BK;
   constexpr uint32_t TCOLS = TOK < 32 ? 32 : TOK;
   __shared__ uint64_t full[MAX_STAGES], empty[MAX_STAGES], acc_full;
   __shared__ uint32_t tmem_base_s, failed;
   __shared__ __align__(16) float s_x[TOK];
   const int tid = threadIdx.x, warp = uniform_warp(), lane = tid & 31;
   const int rank = blockIdx.x % split, tile = blockIdx.x / split;
-  const int n0 = tile % tiles_n * CH, m0 = tile / tiles_n * TOK, all = (a.K + BK - 1) / BK;
+  const int n0 = tile % tiles_n * CHN, m0 = tile / tiles_n * TOK, all = (a.K + BK - 1) / BK;
   const int k0 = all * rank / split, nk = all * (rank + 1) / split - k0;   // (at least one chunk each)
   if (tid == 0) {
     for (int s = 0; s < NS; ++s) {
@@ -133,7 +134,7 @@ k_token_linear(const __grid_constant__ CUtensorMap tma_w, const __grid_constant_
       }
     }
   } else if (warp == 5) {
-    const uint32_t idesc = umma_idesc_i8(CH, TOK), on = elect_one();
+    const uint32_t idesc = umma_idesc_i8(CHN, TOK), on = elect_one();
     bool ready = mbar_test(&full[0], 0);
     int s = 0;
     uint32_t ph = 0;
@@ -173,24 +174,27 @@ k_token_linear(const __grid_constant__ CUtensorMap tma_w, const __grid_constant_
     record_timeout(a.status);
     failed = 1;
   }
-  const int ch = warp * 32 + lane, n = n0 + ch;
+  // 64 rows of an accumulator lie in the first 16 lanes of each warp's 32
+  const int ch = warp * (CHN / 4) + lane % (CHN / 4), n = n0 + ch;
+  const bool mine = (CHN == CH || lane < CHN / 4) && n < a.N;
   __syncwarp();
   if (split > 1) {
     const int log_each = 31 - __clz(TOK / split);
     cluster_arrive();
     cluster_wait();                  // every CTA's products are done (or given up, with its copies landed): its ring may be written to
     const int each = TOK / split;    // tokens that a CTA finishes
-    const uint32_t to = smem_u32(part) + (uint32_t)(rank * each * CH) * 4;
+    const uint32_t to = smem_u32(part) + (uint32_t)(rank * each * CHN) * 4;
     if (warp < 4) {
 #pragma unroll
       for (int c0 = 0; c0 < TOK; c0 += 16) {
         int r[16];
         tmem_ld(tmem + ((uint32_t)(warp * 32) << 16) + c0, r);
         tmem_ld_wait();
+        if (!mine) continue;
         if (each >= 4) {
 #pragma unroll
           for (int i = 0; i < 16; i += 4)
-            st_cluster(cluster_addr_of(to + (uint32_t)(((c0 + i) & (each - 1)) * CH + 4 * ch) * 4, (c0 + i) >> log_each), r[i], r[i + 1], r[i + 2], r[i + 3]);
+            st_cluster(cluster_addr_of(to + (uint32_t)(((c0 + i) & (each - 1)) * CHN + 4 * ch) * 4, (c0 + i) >> log_each), r[i], r[i + 1], r[i + 2], r[i + 3]);
         } else {                     // each is 2
 #pragma unroll
           for (int i = 0; i < 16; i += 2) st_cluster(cluster_addr_of(to + (uint32_t)(2 * ch) * 4, (c0 + i) >> 1), r[i], r[i + 1]);
@@ -202,7 +206,7 @@ k_token_linear(const __grid_constant__ CUtensorMap tma_w, const __grid_constant_
     __syncwarp();
     cluster_arrive();
     cluster_wait();
-    if (warp < 4 && n < a.N && *reinterpret_cast<volatile uint32_t*>(&failed) == 0) {
+    if (warp < 4 && mine && *reinterpret_cast<volatile uint32_t*>(&failed) == 0) {
       const int first = rank * each;
       const float sw = __ldg(a.w_scale + n), b = a.bias ? __ldg(a.bias + n) : 0.0f;
       T* out = static_cast<T*>(a.out) + (long long)(m0 + first) * a.ldo + n;
@@ -215,7 +219,7 @@ k_token_linear(const __grid_constant__ CUtensorMap tma_w, const __grid_constant_
           int4 sum = make_int4(0, 0, 0, 0);
 #pragma unroll 4
           for (int p = 0; p < split; ++p) {
-            const int4 v = *reinterpret_cast<const int4*>(part + (p * each + c) * CH + 4 * ch);
+            const int4 v = *reinterpret_cast<const int4*>(part + (p * each + c) * CHN + 4 * ch);
             sum.x += v.x;
             sum.y += v.y;
             sum.z += v.z;
@@ -231,7 +235,7 @@ k_token_linear(const __grid_constant__ CUtensorMap tma_w, const __grid_constant_
         int2 sum = make_int2(0, 0);
 #pragma unroll 8
         for (int p = 0; p < split; ++p) {
-          const int2 v = *reinterpret_cast<const int2*>(part + p * 2 * CH + 2 * ch);
+          const int2 v = *reinterpret_cast<const int2*>(part + p * 2 * CHN + 2 * ch);
           sum.x += v.x;
           sum.y += v.y;
         }
@@ -240,9 +244,9 @@ k_token_linear(const __grid_constant__ CUtensorMap tma_w, const __grid_constant_
       }
     }
   } else if (warp < 4) {
-    const float sw = n < a.N ? __ldg(a.w_scale + n) : 0.0f, b = a.bias && n < a.N ? __ldg(a.bias + n) : 0.0f;
+    const float sw = mine ? __ldg(a.w_scale + n) : 0.0f, b = a.bias && mine ? __ldg(a.bias + n) : 0.0f;
     store_columns<T, TOK>(tmem + ((uint32_t)(warp * 32) << 16), static_cast<T*>(a.out) + (long long)m0 * a.ldo + n, a.ldo, s_x, sw, b,
-                          ok && n < a.N ? a.M - m0 : 0, [] {});
+                          ok && mine ? a.M - m0 : 0, [] {});
   }
   __syncwarp();
   tc_fence_before();
@@ -423,8 +427,8 @@ int clusters_at_once(int size) {
     c.attrs = &at;
     c.numAttrs = 1;
     int n = 0;
-    if (allow_smem(k_token_linear<32, float>, RING_SM + 1024, configured_on) != cudaSuccess ||
-        cudaOccupancyMaxActiveClusters(&n, k_token_linear<32, float>, &c) != cudaSuccess || n <= 0) {
+    if (allow_smem(k_token_linear<32, CH, float>, RING_SM + 1024, configured_on) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, k_token_linear<32, CH, float>, &c) != cudaSuccess || n <= 0) {
       (void)cudaGetLastError();      // (a guess does as well)
       return sm_count() * 3 / 4 / size;
     }
@@ -439,23 +443,23 @@ int ctas_of_sm(long long tiles, int split) {
   return (int)((tiles + at_once - 1) / at_once);
 }
 
-template <int TOK, typename T>
+template <int TOK, int CHN, typename T>
 cudaError_t launch_tile(const TokenLinearArgs& a, int split, cudaStream_t s) {
   static bool configured_on[MAX_DEVICES];
-  cudaError_t e = allow_smem(k_token_linear<TOK, T>, RING_SM + 1024, configured_on);
+  cudaError_t e = allow_smem(k_token_linear<TOK, CHN, T>, RING_SM + 1024, configured_on);
   if (e != cudaSuccess) return e;
   CUtensorMap tw, tx;
-  if (!make_tmap_i8(&tw, a.wq, a.K, a.N, a.K, CH) || !make_tmap_i8(&tx, a.xq, a.K, a.M, a.K, TOK)) return cudaErrorInvalidValue;
-  const int tiles_n = (a.N + CH - 1) / CH, tiles_m = (a.M + TOK - 1) / TOK;
+  if (!make_tmap_i8(&tw, a.wq, a.K, a.N, a.K, CHN) || !make_tmap_i8(&tx, a.xq, a.K, a.M, a.K, TOK)) return cudaErrorInvalidValue;
+  const int tiles_n = (a.N + CHN - 1) / CHN, tiles_m = (a.M + TOK - 1) / TOK;
   // the CTAs of an SM share the room for rings; a ring needs no more stages than its part of K has chunks, but holds the sums of a split
   const long long ctas = (long long)tiles_n * tiles_m * split;
   const int each = ctas_of_sm((long long)tiles_n * tiles_m, split);
   const int on_sm = each < blocks_per_sm(TOK) ? each : blocks_per_sm(TOK), chunks = ((a.K + BK - 1) / BK + split - 1) / split;
-  int ns = (int)((RING_SM - 1024 * on_sm) / on_sm / stage_bytes(TOK));
+  int ns = (int)((RING_SM - 1024 * on_sm) / on_sm / stage_bytes(TOK, CHN));
   ns = ns < chunks ? ns : chunks;
   ns = ns < 4 ? 4 : ns > MAX_STAGES ? MAX_STAGES : ns;
-  const size_t bytes = (size_t)ns * stage_bytes(TOK) + 1024;
-  return launch_ex(k_token_linear<TOK, T>, dim3((unsigned)ctas), dim3(192), bytes, s, true, (unsigned)split, tw, tx, a, tiles_n, split, ns);
+  const size_t bytes = (size_t)ns * stage_bytes(TOK, CHN) + 1024;
+  return launch_ex(k_token_linear<TOK, CHN, T>, dim3((unsigned)ctas), dim3(192), bytes, s, true, (unsigned)split, tw, tx, a, tiles_n, split, ns);
 }
 template <int PT, typename T>
 cudaError_t launch_pair(const TokenLinearArgs& a, cudaStream_t s) {
@@ -481,13 +485,13 @@ cudaError_t launch_pair(const TokenLinearArgs& a, cudaStream_t s) {
 // for 16 to 64 tokens (16 bytes a store; single words took 1.2 to 3.4), and pays where few tiles have a long K (16 x 1024 x 4096:
 // 5.6 -> 3.6, 256 x 1024 x 14000: 18 -> 10.9).
 double memory_time(const TokenLinearArgs& a, int bytes) { return ((double)a.N * a.K + (double)a.M * a.K + (double)a.M * a.N * bytes) / 6.2e6; }
-double single_cost(const TokenLinearArgs& a, int tok, int split, int bytes) {
-  const double chunk = tok == 16 ? 0.125 : tok == 32 ? 0.13 : 0.183;
+double single_cost(const TokenLinearArgs& a, int tok, int chn, int split, int bytes) {
+  const double chunk = chn == 128 ? (tok == 16 ? 0.125 : tok == 32 ? 0.13 : 0.183) : (tok == 16 ? 0.11 : tok == 32 ? 0.116 : 0.155);
   const double joined = split == 1 ? 0.0 : tok == 16 ? 1.0 : tok == 32 ? 1.5 : 2.2;
   const int chunks = ((a.K + BK - 1) / BK + split - 1) / split;
-  const double each = ctas_of_sm((long long)((a.N + CH - 1) / CH) * ((a.M + tok - 1) / tok), split);
+  const double each = ctas_of_sm((long long)((a.N + chn - 1) / chn) * ((a.M + tok - 1) / tok), split);
   const double memory = memory_time(a, bytes), sums = each * chunks * chunk + (each - 1.0) * 0.024 * tok;
-  return 2.1 + joined + (memory > sums ? memory : sums);
+  return (chn == 128 ? 2.1 : 2.05) + joined + (memory > sums ? memory : sums);
 }
 // A pair: a chunk for both its CTAs' 256 x 256 or 256 x 128; rounds of tiles behind the first at least their epilogue.
 double pair_cost(const TokenLinearArgs& a, int tok, int bytes) {
@@ -497,22 +501,31 @@ double pair_cost(const TokenLinearArgs& a, int tok, int bytes) {
   return (tok == 256 ? 4.8 : 4.55) + (memory > sums ? memory : sums);
 }
 
+template <int CHN, typename T>
+cudaError_t launch_single(const TokenLinearArgs& a, int tok, int split, cudaStream_t s) {
+  return tok == 16   ? launch_tile<16, CHN, T>(a, split, s)
+         : tok == 32 ? launch_tile<32, CHN, T>(a, split, s)
+                     : launch_tile<64, CHN, T>(a, split, s);
+}
 template <typename T>
 cudaError_t launch_typed(const TokenLinearArgs& a, cudaStream_t s) {
   const int chunks = (a.K + BK - 1) / BK;
   double least = 1e300;
-  int tok = 0, split = 1;
+  int tok = 0, chn = CH, split = 1;
   for (int t = 16; t <= 64; t *= 2) {
     if (t == 16 ? a.M > 16 : t / 2 >= a.M) continue;                  // (more tiles of 16 tokens never paid)
-    const long long tiles = (long long)((a.N + CH - 1) / CH) * ((a.M + t - 1) / t);
-    if (tiles > INT32_MAX / 2) continue;
-    for (int p = 1; p <= 8; p *= p == 1 ? 4 : 2) {                    // two chunks at least for each part
-      if (p > 1 && (chunks < 2 * p || ctas_of_sm(tiles, p) > blocks_per_sm(t))) break;
-      const double c = single_cost(a, t, p, sizeof(T));
-      if (c < least || (c == least && t > tok)) {
-        least = c;
-        tok = t;
-        split = p;
+    for (int n = 64; n <= CH; n *= 2) {
+      const long long tiles = (long long)((a.N + n - 1) / n) * ((a.M + t - 1) / t);
+      if (tiles > (n == CH ? INT32_MAX / 2 : sm_count())) continue;   // (tiles of 64 channels: for SMs that would be idle)
+      for (int p = 1; p <= 8; p *= p == 1 ? 4 : 2) {                  // two chunks at least for each part
+        if (p > 1 && (chunks < 2 * p || ctas_of_sm(tiles, p) > blocks_per_sm(t))) break;
+        const double c = single_cost(a, t, n, p, sizeof(T));
+        if (c < least || (c == least && t >= tok)) {
+          least = c;
+          tok = t;
+          chn = n;
+          split = p;
+        }
       }
     }
   }
@@ -523,11 +536,9 @@ cudaError_t launch_typed(const TokenLinearArgs& a, cudaStream_t s) {
       tok = t;
     }
   }
-  return tok == 16    ? launch_tile<16, T>(a, split, s)
-         : tok == 32  ? launch_tile<32, T>(a, split, s)
-         : tok == 64  ? launch_tile<64, T>(a, split, s)
-         : tok == 128 ? launch_pair<128, T>(a, s)
-                      : launch_pair<256, T>(a, s);
+  return tok > 64 || tok == 0 ? (tok == 128 ? launch_pair<128, T>(a, s) : launch_pair<256, T>(a, s))
+         : chn == CH          ? launch_single<CH, T>(a, tok, split, s)
+                              : launch_single<64, T>(a, tok, split, s);
 }
 
 }  // namespace

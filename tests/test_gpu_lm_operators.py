@@ -227,7 +227,8 @@ def test_linear_of_many_tiles(Bd, M, N, K, dtype):
 
 
 @pytest.mark.parametrize("M,N,K", [(13, 2000, 4100), (5, 259, 2050), (250, 130, 4100), (400, 130, 9003), (29, 100, 4100), (51, 1021, 14000),
-                                   (400, 259, 6000), (250, 130, 14000), (200, 1000, 6000), (128, 512, 8192), (9, 5000, 14000), (30, 5100, 14000)])
+                                   (400, 259, 6000), (250, 130, 14000), (200, 1000, 6000), (128, 512, 8192), (9, 5000, 14000), (30, 5100, 14000),
+                                   (16, 4097, 2048), (32, 4100, 4096), (60, 4095, 4096), (128, 1025, 2048), (30, 1021, 2048), (3, 65, 4096)])
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_linear_of_few_tiles_and_a_long_sum(Bd, M, N, K, dtype):
     # 16, 32 and 64 tokens a tile, each of whose sums is shared by 4 or 8 CTAs
