@@ -240,10 +240,12 @@ __device__ __forceinline__ void pack(Vec<__nv_bfloat16>& v, const float (&f)[8])
 // the row a thread.  WHOLE: rows are 16-byte aligned and a multiple of that long.
 // Long rows are bound by memory (4096 x 4096 with a residual: fp32 36.9 us, 5.9 TB/s; bf16 24.4 us, 4.8 TB/s), short ones of 16 bits
 // by their instructions, about 14 for each element, and waits that few warps cover (16000 x 1280 fp16 alone: 18.0 us, 3.4 TB/s; with a
-// sixth vector that holds nothing 20.6; with the next row copied ahead to shared memory 22).  One warp a row needs no barrier; wider groups take rows that a warp's registers do not hold, and few rows, where a row's latency is the call's (16 x 1024: 2.2 us).
+// sixth vector that holds nothing 20.6; with the next row copied ahead to shared memory 22).  One warp a row needs no barrier;
+// wider groups take rows that a warp's registers do not hold, and few rows, where a row's latency is the call's (16 x 1024: 2.2 us).
 // Forming the products again for the codes, for registers of half as many bits, took 10 % more.  Rows that are not 16-byte
 // aligned (4096 x 4001 bf16) take 49 us; element by element they took 75.
-// Threads of a block: four rows of one warp, or one row.  Blocks of an SM: 64 registers a thread for up to 16 elements, 80 for up to 40, 96 and 128 for up to 48 and 64
+// Threads of a block: four rows of one warp, or one row.  Blocks of an SM: 64 registers a thread for up to 16 elements, 80 for up to
+// 40, 96 and 128 for up to 48 and 64.
 __host__ __device__ constexpr int norm_threads(int threads) { return threads > 32 ? threads : 128; }
 __host__ __device__ constexpr int norm_blocks(int threads, int elements) {
   return 128 * (elements <= 16 ? 8 : elements <= 40 ? 6 : elements <= 48 ? 5 : 4) / norm_threads(threads);
