@@ -428,7 +428,8 @@ int q4_feature_prologue(const float* mel, int32_t B, int32_t T100, int32_t M, vo
  *   MAX boundary alpha = max |y_i| (1 for a row of zeros), scale_out = alpha / 127, code_i = y_i / scale_out rounded to the
  *   nearest integer, halves to even.  The root is a common factor of the row: codes are those of
  *   127 h_i gain_i / max |h gain|, decided in double where fp32 cannot tell, so they do not depend on the order of the sum.
- * A row that holds a NaN or an infinity gets codes 0 and a NaN scale.  Values of any finite magnitude are accepted.
+ * A row that holds a NaN or an infinity, or whose product with the gain does (a gain that is not finite does so to every row), gets
+ * codes 0 and a NaN scale.  Values of any finite magnitude are accepted.
  *   x [rows, k] dtype, row stride x_stride; residual (nullable) and sum_out (required with residual, refused without)
  *   likewise; sum_out may be x or residual itself (same pointer and stride).  gain [k] fp32, 16-byte aligned.  0 <= eps, finite.
  *   q_out [rows, k_pad] codes as for quantize_pack_int4 (k_pad a multiple of 32, elements behind k are 0); scale_out [rows].

@@ -132,13 +132,20 @@ __device__ __forceinline__ void store_codes(int8_t* q, const int (&c)[N]) {
     *reinterpret_cast<uint32_t*>(q) = w[0];
 }
 
+__device__ __forceinline__ float larger(float a, float b) {   // a NaN stays
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+__device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
+
 // Sum and maximum over the THREADS threads of a row, the same in all of them.
 template <int THREADS, typename F>
 __device__ __forceinline__ void row_reduce(F& sum, F& top, F (*s)[2]) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    top = larger(top, __shfl_xor_sync(0xffffffffu, top, o));
   }
   if (THREADS > 32) {
     if ((threadIdx.x & 31) == 0) {
@@ -150,7 +157,7 @@ __device__ __forceinline__ void row_reduce(F& sum, F& top, F (*s)[2]) {
 #pragma unroll
     for (int w = 0; w < THREADS / 32; ++w) {
       sum += s[w][0];
-      top = max(top, s[w][1]);
+      top = larger(top, s[w][1]);
     }
     __syncthreads();
   }
@@ -193,9 +200,9 @@ __device__ __noinline__ void norm_row(const NormArgs& a, long long row, int t, d
 constexpr float MAGIC = 12582912.0f;   // 1.5 * 2^23: adding it leaves the nearest integer in the low bits
 constexpr float SETTLED = 0.5f - 3.2e-5f;
 
-__device__ __forceinline__ float max_abs3(float a, float b, float c) {   // of the magnitudes
+__device__ __forceinline__ float max_abs3(float a, float b, float c) {   // of the magnitudes, a NaN stays
   float d;
-  asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
 
@@ -316,7 +323,8 @@ __global__ void __launch_bounds__(norm_threads(THREADS), norm_blocks(THREADS, NV
       sum += odd;
     }
     row_reduce<THREADS>(sum, top, s_part);
-    if (!(top > 1e-30f && top < 1e37f && sum > 1e-30f && sum < 1e38f)) {   // (a NaN or infinity is in the sum)
+    // (a NaN or infinity of the row is in the sum, one of the gain, or of both, in the maximum)
+    if (!(top > 1e-30f && top < 1e37f && sum > 1e-30f && sum < 1e38f)) {
       norm_row<T, THREADS>(a, row, t, s_part64);
       continue;
     }
