@@ -427,7 +427,8 @@ int q4_feature_prologue(const float* mel, int32_t B, int32_t T100, int32_t M, vo
  *   y_i = h_i * gain_i / sqrt(mean(h^2) + eps);
  *   MAX boundary alpha = max |y_i| (1 for a row of zeros), scale_out = alpha / 127, code_i = y_i / scale_out rounded to the
  *   nearest integer, halves to even.  The root is a common factor of the row: codes are those of
- *   127 h_i gain_i / max |h gain|, decided in double where fp32 cannot tell, so they do not depend on the order of the sum.
+ *   127 h_i gain_i / max |h gain| in exact arithmetic (decided in double where fp32 cannot tell, exact halves by exact products), so
+ *   they do not depend on the order of the sum.
  * A row that holds a NaN or an infinity, or whose product with the gain does (a gain that is not finite does so to every row), gets
  * codes 0 and a NaN scale.  Values of any finite magnitude are accepted.
  *   x [rows, k] dtype, row stride x_stride; residual (nullable) and sum_out (required with residual, refused without)

@@ -6,8 +6,8 @@
 //
 // Codes are those of exact arithmetic.  In fp32 t = v (127 / max |v|) is off by at most three roundings, 127 * 3 * 2^-24 < 2.3e-5; an
 // element whose t lies further than that from a half is decided by it (t is not rounded itself: a fused operation adds the number
-// that leaves its nearest integer, another takes the distance).  The others are decided in double, where v is exact
-// and a half is met exactly; the maximum is then taken from the exact products too.
+// that leaves its nearest integer, another takes the distance).  The others are decided in double, where v is exact and a half is
+// decided by exact products (exact_code); the maximum is then taken from the exact products too.
 #include <cuda_bf16.h>
 
 #include "q4_internal.h"
@@ -167,6 +167,23 @@ __device__ __forceinline__ bool row_any(bool v) {
   return THREADS > 32 ? __syncthreads_or(v) != 0 : __any_sync(0xffffffffu, v) != 0;
 }
 
+// 127 v / top rounded to the nearest integer, halves to even; v and top are products of two fp32 values, of 48 bits at most.  Of the
+// quotient only its last bits are uncertain (by 127 * 3 * 2^-53), so that it decides unless it lies within 10^-9 of some n + 1/2, where the
+// sign of 254 |v| - (2 n + 1) top does.  Those products take up to
+// 56 bits: each is a rounded one and what fused operations find it to lack.  The rounded ones lie within 2 % of each other, so that their
+// difference is exact, and so is that of the lacks, a few of their last places; one rounding of the sum keeps the sign.
+__device__ __forceinline__ int exact_code(double v, double top) {
+  constexpr double MAGIC64 = 6755399441055744.0;   // 1.5 * 2^52: adding it leaves the nearest integer in the low bits
+  const double q = 127.0 * v / top, m = __dadd_rn(q, MAGIC64);
+  if (fabs(q - (m - MAGIC64)) < 0.5 - 1e-9) return __double2loint(m);
+  const double size = fabs(v);
+  const int n = (int)fabs(q);
+  const double odd = 2 * n + 1, a = __dmul_rn(254.0, size), b = __dmul_rn(odd, top);   // (rounded: not fused with what follows)
+  const double over = (a - b) + (fma(254.0, size, -a) - fma(odd, top, -b));
+  const int code = n + (over > 0.0 || (over == 0.0 && (n & 1)));
+  return v < 0.0 ? -code : code;
+}
+
 // A row in double, from memory: for rows that hold no more than zeros, a NaN or infinity, or values whose squares or products leave
 // the range of fp32, and for rows too long for registers.  Elements vec, vec + THREADS, ... of N are thread `t`'s, as everywhere.
 template <typename T, int THREADS>
@@ -190,7 +207,7 @@ __device__ __noinline__ void norm_row(const NormArgs& a, long long row, int t, d
     int c[N];
     for (int i = 0; i < N; ++i) {
       const int at = v * N + i;
-      c[i] = at < a.k && !bad && top > 0.0 ? __double2int_rn(127.0 * ((double)to_f32<T>(h[at]) * (double)a.gain[at]) / top) : 0;
+      c[i] = at < a.k && !bad && top > 0.0 ? exact_code((double)to_f32<T>(h[at]) * (double)a.gain[at], top) : 0;
     }
     store_codes<N>(q + v * N, c);
   }
@@ -369,7 +386,7 @@ __global__ void __launch_bounds__(norm_threads(THREADS), norm_blocks(THREADS, NV
         const int at = (t + j * THREADS) * N + i;
         if (at >= a.k) break;
         const float f = to_f32<T>(h[at]), g = a.gain[at], p = __fmul_rn(f, g), m = __fmaf_rn(p, inv, MAGIC);
-        if (fabsf(__fmaf_rn(p, inv, __fsub_rn(MAGIC, m))) > SETTLED) q[at] = (int8_t)__double2int_rn(127.0 * ((double)f * (double)g) / exact);
+        if (fabsf(__fmaf_rn(p, inv, __fsub_rn(MAGIC, m))) > SETTLED) q[at] = (int8_t)exact_code((double)f * (double)g, exact);
       }
     }
   }

@@ -1,4 +1,5 @@
 """The operators around a language model's output where a first set of tests did not look."""
+from fractions import Fraction
 
 import pytest
 import torch
@@ -42,3 +43,54 @@ def test_norm_with_a_gain_that_is_not_finite(Bd, dtype, rows, k, at, gain_at):
             assert torch.equal(out.cpu(), (x.float() + r.float()).to(dtype))
     codes, scale = Bd.q4_rmsnorm_quantize(x.cuda(), sound.cuda(), 1e-5)     # (the row itself is a sound one)
     assert torch.isfinite(scale).all()
+
+
+def code_of(h, gain, top):
+    """127 h gain / top rounded to the nearest integer, halves to even, in rational numbers (fp32 values are such)."""
+    return round(127 * Fraction(h) * Fraction(gain) / top)
+
+
+def check_codes_in_rationals(Bd, x, gain, pad):
+    """x [rows, m] with m gains, in rows of `pad` elements whose others are zeros."""
+    rows, m = x.shape
+    wide, wide_gain = torch.zeros(rows, pad), torch.ones(pad)
+    wide[:, :m], wide_gain[:m] = x, gain
+    codes, scale = Bd.q4_rmsnorm_quantize(wide.cuda(), wide_gain.cuda(), 1e-5)
+    got = codes.cpu().view(torch.int8)
+    xs, gs = x.tolist(), gain.tolist()
+    for i in range(rows):
+        top = max(abs(Fraction(h) * Fraction(f)) for h, f in zip(xs[i], gs))
+        assert got[i, :m].tolist() == [code_of(h, f, top) for h, f in zip(xs[i], gs)]
+    assert (got[:, m:] == 0).all() and torch.isfinite(scale).all()
+
+
+# rows that fit a warp, wider groups, and rows from memory; and rows from memory because squares leave fp32
+@pytest.mark.parametrize("pad,factor", [(256, 1.0), (1001, 1.0), (9000, 1.0), (20011, 1.0), (256, 2.0 ** 66)])
+def test_norm_of_exact_halves_with_long_mantissas(Bd, pad, factor):
+    # h = (2n+1) a beside 254 a: 127 h / max is n + 1/2 whatever the gain, though h gain takes 48 bits and 127 of them 55
+    g = gen(pad)
+    a = 2 * torch.randint(1 << 14, 1 << 15, (24, 1), generator=g) + 1
+    sign = 1 - 2 * torch.randint(0, 2, (24, 127), generator=g)
+    x = torch.cat([254 * a, (2 * torch.arange(127) + 1) * a * sign], 1).double()
+    assert torch.equal(x.float().double(), x)
+    for gain in (1.0580815, 0.70710677, 1.9999999, 3.0):
+        check_codes_in_rationals(Bd, x.float() * factor, torch.full((128,), gain), pad)
+
+
+@pytest.mark.parametrize("pad", [256, 20011])
+def test_norm_of_fp32_next_to_halves(Bd, pad):
+    # products a step of their last bits beside a half: (y - 1)(y + 1) = y^2 - 1 against y^2
+    g = gen(pad)
+    y = torch.randint(1 << 14, (1 << 16) - 2, (8, 1), generator=g).double()
+    n = 2 * torch.arange(60).double() + 1
+    below, above = n * (y - 1), n * y                         # times y + 1 and y
+    for row in range(8):
+        v = float(y[row])
+        # max 254 y^2: n (y^2 - 1) lies below the half, n y^2 on it; max 254 (y^2 - 1): n (y^2 - 1) on it, n y^2 above it
+        for top, top_gain in ((254 * v, v), (254 * (v - 1), v + 1)):
+            x = torch.cat([torch.tensor([top], dtype=torch.float64), below[row], -above[row]])[None]
+            gain = torch.cat([torch.tensor([top_gain], dtype=torch.float64), torch.full((60,), v + 1, dtype=torch.float64),
+                              torch.full((60,), v, dtype=torch.float64)])
+            assert torch.equal(x.float().double(), x)
+            check_codes_in_rationals(Bd, x.float(), gain.float(), pad)
+    check_codes_in_rationals(Bd, torch.randn(20, 120, generator=g), torch.randn(120, generator=g), pad)
