@@ -289,7 +289,9 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
   if (tid == 0) sh.n = sh.noted = 0;
 
   float m = first != first ? -INFINITY : first, scale = sum_scale(m), bound = -INFINITY, limit = -INFINITY;
-  float sum = exp2_unit(__fmaf_rn(first, LOG2E, -scale));   // (a NaN makes the sum NaN)
+  // A turn's 16 or 32 terms are added in fp32, four chains of them, turns in double: 10 roundings of 2^-24 at most, where fp32 alone
+  // would add one a turn.  (A NaN makes the sum NaN.)
+  double sum = exp2_unit(__fmaf_rn(first, LOG2E, -scale));
   auto turn = [&](const uint4 (&raw)[ROW_VECTORS], int t) {
     float vector_top[ROW_VECTORS], top = -INFINITY;
 #pragma unroll
@@ -329,7 +331,7 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
     }
     float even, odd;
     upk2(add2(part_sum[0], part_sum[1]), even, odd);
-    sum = sum * pow2_down(scale - now) + (even + odd);
+    sum = fma(sum, (double)pow2_down(scale - now), (double)(even + odd));
     scale = now;
   };
   for (int t = 0; t < turns; t += 2) {   // two sets of registers: one on its way, one worked on
@@ -341,7 +343,7 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
   }
   m = fmaxf(m, last);
   const float now = sum_scale(m);
-  sum = sum * pow2_down(scale - now) + exp2_unit(__fmaf_rn(last, LOG2E, -now));
+  sum = fma(sum, (double)pow2_down(scale - now), (double)exp2_unit(__fmaf_rn(last, LOG2E, -now)));
   scale = now;
 
   // candidates: elements that reach the last bound (without turns there is none)
@@ -374,7 +376,7 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
     most = fmaxf(most, sh.scale[w]);
   }
   const bool far = top > -INFINITY && fabsf(top) > 1e6f;
-  double total = (double)(sum * pow2_down(scale - most));
+  double total = sum * (double)pow2_down(scale - most);
   const int from = part == 0 ? 0 : head + v0 * N, to = part + 1 == p.parts ? a.V : head + v1 * N;
   if (far) {   // differences from the maximum, which are exact where they count
     total = 0.0;

@@ -1,6 +1,7 @@
 """The operators around a language model's output where a first set of tests did not look."""
 from fractions import Fraction
 
+import numpy as np
 import pytest
 import torch
 
@@ -94,3 +95,21 @@ def test_norm_of_fp32_next_to_halves(Bd, pad):
             assert torch.equal(x.float().double(), x)
             check_codes_in_rationals(Bd, x.float(), gain.float(), pad)
     check_codes_in_rationals(Bd, torch.randn(20, 120, generator=g), torch.randn(120, generator=g), pad)
+
+
+# ----------------------------------------------------------------------------------------------------------- select
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_select_adds_many_small_terms_to_a_large_sum(Bd, dtype):
+    # A row of 16 turns, one segment: every thread meets terms of 1 first, then 15 turns whose terms are each below half of the last
+    # fp32 place of its sum so far, 8e-7 of it together.  Terms of 1 are exact (2^0), the small ones good to 1e-6 of themselves, and
+    # what is added to a sum in double stays; the scores lie near 0, where fp32 shows it.
+    per, B, W = (2048, 33, 32) if dtype == torch.float32 else (4096, 33, 32)      # elements of a turn; more rows than block slots
+    z = torch.full((B, W, 16 * per), -16.75, dtype=dtype, device="cuda")
+    z[:, :, :per] = 0
+    lse = float(np.log(per + 15 * per * np.exp(-16.75)))
+    score = torch.full((B, W), round(lse * 64) / 64, device="cuda") - torch.arange(W, device="cuda") / 64
+    r = Bd.q4_lm_beam_select(z, score)
+    want = score[0, 0].double().item() - lse
+    assert abs(want) < 2.0 ** -6                              # rounded to fp32 by less than 2^-31
+    assert (r["parent"] == 0).all() and (r["token"].cpu() == torch.arange(W)).all()
+    assert ((r["score"].double() - want).abs() < 1e-9).all(), (r["score"].double() - want).abs().max().item()
