@@ -466,7 +466,8 @@ int q4_linear_token_scales(const void* xq, const float* x_scale, int32_t M, cons
  * A logit of -inf is a label that is not proposed.  A row that holds a NaN or +inf, or nothing but -inf, proposes nothing.
  * Whatever dtype is: exponentials are formed in fp32 and added in fp32 by 16 or 32, those sums, scores and comparisons are carried
  * out in double.  A row's log sum exp is off by 5e-6 at the very most; proposals of different beams that lie closer than that may
- * come out in either order.  Proposals whose score lies outside the range of fp32 are none.  W <= 32, V < 2^31.  No output may be an input.
+ * come out in either order (beams of equal scores and equal rows have equal proposals, wherever their rows begin).  Proposals whose
+ * score lies outside the range of fp32 are none.  W <= 32, V < 2^31.  No output may be an input.
  *   arrived [B (W + 1)]: counters, zero before the first call; every call leaves them zero.  workspace: q4_workspace_bytes(
  *   Q4_WS_LM_SELECT, {B, W, V}) bytes, any contents.  Calls that may overlap need counters and a workspace each.
  */

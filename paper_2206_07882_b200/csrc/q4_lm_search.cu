@@ -150,6 +150,7 @@ struct RowShared {            // of a segment
 struct MergeShared {
   double base[MAX_BEAMS], lse[MAX_BEAMS];   // score + rho and log-sum-exp of a beam's row; an ended beam's score
   int32_t kind[MAX_BEAMS];                  // 0: the beam proposes nothing, 1: labels, 2: it has ended
+  uint32_t like[MAX_BEAMS], any_like;       // earlier beams whose rows may be equal; beams that have any
   long long key[MERGE_LIST];
   float z[MERGE_LIST];
   int32_t label[MERGE_LIST], beam[MERGE_LIST], pick[MERGE_LIST];
@@ -461,14 +462,36 @@ __device__ __forceinline__ void merge_row(const RowParts& p, long long row, int 
   }
 }
 
-// How far sums of the same row may lie apart (terms off by 2^-22, chains of 64 roundings)
-constexpr double SAME_SUM = 4.2e-6;
+// How far sums of equal rows may lie apart: each is off by less than 5e-6 (terms by 2^-22 and by what rounds their arguments, 10
+// roundings of 2^-24, the same again where segments are joined)
+constexpr double SAME_SUM = 1e-5;
+
+// Whether two rows hold the same values, by the whole block.  Only beams that are all but certainly alike come here: 15 us for 50257 labels
+// (1 x 32 x 50257 fp32 with all beams alike 400 us, with none 22).  More loads under way at a time cost registers that every row would miss.
+template <typename T>
+__device__ __forceinline__ bool same_rows(const T* x, const T* y, int V) {
+  constexpr int EACH = 8;
+  bool same = true;
+  for (int left = V - (int)threadIdx.x; left > 0 && same; left -= left > ROW_NT * EACH ? ROW_NT * EACH : left) {
+    const T *xs = x + (V - left), *ys = y + (V - left);
+    T u[EACH], v[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      u[i] = i * ROW_NT < left ? xs[i * ROW_NT] : T(0.0f);
+      v[i] = i * ROW_NT < left ? ys[i * ROW_NT] : T(0.0f);
+    }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) same = to_f32<T>(u[i]) == to_f32<T>(v[i]) && same;
+  }
+  return __syncthreads_and(same) != 0;
+}
 
 // The W best proposals of an utterance from its rows' lists.  A proposal's score is score[w] + rho + (z - lse) in double (the logits may
 // be far larger than their differences).  As for a segment a bound from group maxima (rounded down to fp32, so it errs on
 // the safe side) leaves few proposals to rank; where the best are in few groups (beams far apart, or many beams alike) it leaves
 // hundreds, and a second bound is taken among those.
 // Double precision is slow to wait for: two additions and two conversions an entry, everything else is done on the keys.
+template <typename T>
 __device__ __forceinline__ void merge_rows(const LmSelectArgs& a, const RowParts& p, int utterance, SelectShared& sh) {
   MergeShared& mg = sh.merge;
   const int tid = threadIdx.x, W = a.W, entries = W * W;   // entry w W + j: place j of beam w
@@ -484,35 +507,43 @@ __device__ __forceinline__ void merge_rows(const LmSelectArgs& a, const RowParts
   if (tid < 32) {
     const float score = tid < W ? a.score[row0 + tid] : -INFINITY;
     const bool ended = tid < W && a.done && a.done[row0 + tid] && isfinite(score);
-    double lse = tid < W ? __ldcg(p.lse + (row0 + tid) * p.parts) : NAN;    // (a beam that is empty or ended left none: not used)
+    const double lse = tid < W ? __ldcg(p.lse + (row0 + tid) * p.parts) : NAN;   // (a beam that is empty or ended left none: not used)
     const bool rows = isfinite(score) && !ended && isfinite(lse);           // (not finite: nothing but -inf, a NaN or +inf)
     // Beams of equal scores and equal rows have equal proposals, but rows that begin at different places of 16 bytes are summed in
-    // another order.  Such a beam takes the sum of the first one like it: same score, same list, and all but the same sum.
-    uint32_t like = __match_any_sync(0xffffffffu, rows ? __float_as_uint(score + 0.0f) : 0x7fc00000u | tid) & ((1u << tid) - 1);
-    const double own = lse;
-    while (__any_sync(0xffffffffu, like != 0)) {
-      const int w = like ? __ffs(like) - 1 : tid;
-      const double other = __shfl_sync(0xffffffffu, own, w);
-      if (like == 0) continue;
-      like &= like - 1;
-      if (!(fabs(own - other) <= SAME_SUM)) continue;
-      int j = 0;
-      for (; j < W; ++j) {
-        const Best mine_j = load_best(p.best + (row0 + tid) * p.parts * W + j), other_j = load_best(p.best + (row0 + w) * p.parts * W + j);
-        if (mine_j.value != other_j.value || mine_j.label != other_j.label) break;
-      }
-      if (j < W) continue;
-      lse = other;
-      like = 0;
+    // another order.  Such a beam takes the sum of the first one like it.  Asked for here: same score, another place of 16 bytes, and a
+    // sum that differs, by no more than that makes it; the rows themselves are compared below.
+    uint32_t alike = __match_any_sync(0xffffffffu, rows ? __float_as_uint(score + 0.0f) : 0x7fc00000u | tid) & ((1u << tid) - 1), like = 0;
+    const uint32_t place = (uint32_t)(((row0 + tid) * a.ld * (long long)sizeof(T)) & 15);
+    while (__any_sync(0xffffffffu, alike != 0)) {
+      const int w = alike ? __ffs(alike) - 1 : tid;
+      const double other = __shfl_sync(0xffffffffu, lse, w);
+      const uint32_t other_place = __shfl_sync(0xffffffffu, place, w);
+      if (alike == 0) continue;
+      alike &= alike - 1;
+      if (place != other_place && lse != other && fabs(lse - other) <= SAME_SUM) like |= 1u << w;
     }
     if (tid < W) {
       mg.base[tid] = ended ? (double)score : (double)score + (double)a.rho;
       mg.lse[tid] = lse;
       mg.kind[tid] = ended ? 2 : rows ? 1 : 0;
+      mg.like[tid] = like;
     }
+    like = __ballot_sync(0xffffffffu, like != 0);
+    if (tid == 0) mg.any_like = like;
   }
   if (tid == 0) sh.n = sh.picked = 0;
   __syncthreads();
+  for (uint32_t left = mg.any_like; left; left &= left - 1) {   // seldom any
+    const int w = __ffs(left) - 1;
+    const T* z = static_cast<const T*>(a.logits) + row0 * a.ld;
+    for (uint32_t like = mg.like[w]; like; like &= like - 1) {
+      const int v = __ffs(like) - 1;
+      if (!same_rows(z + w * a.ld, z + v * a.ld, a.V)) continue;
+      if (tid == 0) mg.lse[w] = mg.lse[v];
+      break;
+    }
+    __syncthreads();
+  }
   long long key[EACH], head = NO_PROPOSAL;
 #pragma unroll
   for (int i = 0; i < EACH; ++i) {
@@ -605,7 +636,7 @@ __global__ void __launch_bounds__(ROW_NT, ROW_BLOCKS) k_lm_select(const LmSelect
     if (!last_to_arrive(a.arrived + a.B + row, p.parts, sh)) return;
     if (live) merge_row(p, row, a.W, sh);
   }
-  if (last_to_arrive(a.arrived + utterance, a.W, sh)) merge_rows(a, p, utterance, sh);
+  if (last_to_arrive(a.arrived + utterance, a.W, sh)) merge_rows<T>(a, p, utterance, sh);
 }
 
 // Moves of up to Q4_REORDER_MAX tensors, rows cut into vectors of `width` bytes.  A block takes a piece of one long row or some

@@ -113,3 +113,47 @@ def test_select_adds_many_small_terms_to_a_large_sum(Bd, dtype):
     assert abs(want) < 2.0 ** -6                              # rounded to fp32 by less than 2^-31
     assert (r["parent"] == 0).all() and (r["token"].cpu() == torch.arange(W)).all()
     assert ((r["score"].double() - want).abs() < 1e-9).all(), (r["score"].double() - want).abs().max().item()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("gap", [0, 1, 3])
+@pytest.mark.parametrize("V", [64, 1024, 9000, 70000])
+def test_select_of_beams_that_differ_in_their_tails_only(Bd, dtype, gap, V):
+    # Equal scores and equal best labels, but one row holds a little more beside them: 2e-6 of its sum, several times what terms
+    # and sums are off by (e^-1 by 2^-22 of itself, a handful of roundings of 2^-24).  Each keeps its own sum, the lighter tail wins.
+    W, low = 2, torch.finfo(dtype).min
+    for heavy in (0, 1):
+        z = torch.full((1, W, V + gap), low, dtype=dtype)
+        z[:, :, 3], z[:, :, V - 5] = 0.0, -1.0
+        z[0, :, V // 2] = -16.0
+        z[0, heavy, V // 2] = -12.75
+        score = torch.full((1, W), 0.3125)
+        r = Bd.q4_lm_beam_select(z.cuda()[:, :, :V], score.cuda())
+        total = score.double() - torch.logsumexp(z[:, :, :V].double(), 2)
+        assert (total[0, 1 - heavy] - total[0, heavy]).item() > 1.9e-6
+        assert r["parent"].tolist() == [[1 - heavy, heavy]] and r["token"].tolist() == [[3, 3]]
+        got = r["score"].cpu().double()[0]
+        assert (got - torch.stack([total[0, 1 - heavy], total[0, heavy]])).abs().max() < 8e-7
+        assert 1.6e-6 < (got[0] - got[1]).item() < 2.4e-6
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_select_of_equal_rows_and_of_nearly_equal_ones(Bd, dtype):
+    # rows that begin at different places of 16 bytes: equal ones are told apart by their number, one that differs in its last label
+    # alone is a row of its own (2e-6 of its sum), whether it comes before, between or behind them
+    V, W = 4099, 12
+    g = gen(5)
+    row = torch.full((V,), -30.0)
+    row[torch.randperm(V - 1, generator=g)[:W]] = -torch.arange(W).float() / 8
+    for other in ((0,), (5,), (11,), (2, 7), (0, 11)):
+        z = row.to(dtype).repeat(1, W, 1)
+        for w in other:
+            z[0, w, V - 1] = -11.25                           # 1.3e-5 beside a sum of about 6.6
+        r = Bd.q4_lm_beam_select(z.cuda(), torch.zeros(1, W, device="cuda"))
+        order = [w for w in range(W) if w not in other] + list(other)
+        assert r["parent"].tolist() == [order] and len(set(r["token"][0].tolist())) == 1
+        got = r["score"].cpu()[0]
+        n = W - len(other)
+        assert len(set(got[:n].tolist())) == 1 and (len(set(got[n:].tolist())) == 1)
+        want = -torch.logsumexp(z[0].double(), 1)[order]
+        assert (got.double() - want).abs().max() < 1.3e-6 and got[n - 1] > got[n]
