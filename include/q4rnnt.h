@@ -483,8 +483,10 @@ int q4_lm_beam_select(const void* logits, int64_t logits_stride, int32_t dtype, 
  *   base + i0 step[0] + i1 step[1] + (b W + w) row_step,  i0 < n[0], i1 < n[1]   (bytes; steps of src and dst of their own):
  * n[0] for what lies outside the beams (layers), n[1] for what lies inside (heads), so that the used part of a cache can be
  * moved and the rest left alone.  Steps are not negative, those of dst no shorter than a row.  No dst may overlap a src of the
- * call (Q4_ERR_UNSUPPORTED, judged by the range from a tensor's first to its last byte), and rows of dst lie apart;
- * parent [B, W] (device).
+ * call (Q4_ERR_UNSUPPORTED, judged by the range from a tensor's first to its last byte), and rows of dst lie apart, those of one tensor
+ * from another's too; parent [B, W] (device).
+ * q4_beam_reorder_check: the checks of any number of items as if they were one call; nothing is launched.  For moves of more tensors than
+ * one call takes, before the first of them: the later calls read what the earlier ones have left of their src.
  */
 #define Q4_REORDER_MAX 16
 typedef struct {
@@ -494,6 +496,7 @@ typedef struct {
   int64_t n[2], src_step[2], dst_step[2];
 } q4_reorder;
 int q4_beam_reorder(const q4_reorder* items, int32_t n_items, const int32_t* parent, int32_t B, int32_t W, q4_stream stream);
+int q4_beam_reorder_check(const q4_reorder* items, int32_t n_items, int32_t B, int32_t W);
 
 #define Q4_WS_LSTM_LAYER 1 /* dims = {T, B, dirs, H} or {T, B, dirs, H, kx_pad} */
 #define Q4_WS_JOINT 2      /* dims = {N, D} or {N, D, Hp_pad} (tensor-core path) */

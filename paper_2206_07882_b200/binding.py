@@ -94,7 +94,7 @@ EXPORTS = ["q4_act_symmetric", "q4_act_asymmetric", "quantize_pack_int4", "qlstm
            "dr_fusion_beam_step", "q4_beam_search", "q4_search_plan_create", "q4_search_plan_destroy", "q4_search_plan_info", "q4_search_steps_taken", "q4_traceback", "q4_feature_prologue", "q4_workspace_bytes",
            "q4_poll_status", "q4_version", "q4_launch_count", "q4_dependent_launch_set", "q4_beam_select_exact_set", "q4_timing_set", "q4_timing_count", "q4_prepared_bytes", "q4_prepare_model", "q4_table_bytes", "q4_prepare_tables", "qjoint_logprobs_static", "q4_quantizer_calls", "q4_prepared_lstm_bytes", "q4_prepare_lstm",
            "q4_prepared_linear_bytes", "q4_prepare_linear", "q4_test_wait_expiry_set", "q4_test_search_loop_failure_set", "q4_encoder_time_slicing_set", "q4_encoder_recurrence_plan",
-           "q4_rmsnorm_quantize", "q4_linear_token_scales", "q4_lm_beam_select", "q4_beam_reorder"]
+           "q4_rmsnorm_quantize", "q4_linear_token_scales", "q4_lm_beam_select", "q4_beam_reorder", "q4_beam_reorder_check"]
 
 _lib = None
 
@@ -120,6 +120,7 @@ def lib() -> C.CDLL:
         _lib.q4_linear_token_scales.argtypes = [v, v, i, C.POINTER(Mat), v, v, i, j, v, v]
         _lib.q4_lm_beam_select.argtypes = [v, j, i, v, v, i, i, i, i, f, v, v, v, v, v, v, z, v]
         _lib.q4_beam_reorder.argtypes = [v, i, v, i, i, v]
+        _lib.q4_beam_reorder_check.argtypes = [v, i, i, i]
     return _lib
 
 
@@ -696,7 +697,8 @@ def _reorder_item(src: torch.Tensor, dst: torch.Tensor, dim: int, B: int, W: int
 
 def q4_beam_reorder(pairs: Sequence, parent: torch.Tensor, dim: int = 0):
     """dst[..., b, w, ...] = src[..., b, parent[b, w], ...] for pairs (src, dst) of tensors whose dimensions `dim` and `dim` + 1
-    are utterance and beam; where parent is negative dst is left as it was.  Views are fine (the used part of a cache)."""
+    are utterance and beam; where parent is negative dst is left as it was.  Views are fine (the used part of a cache).  No dst may
+    overlap a src, of whichever pair; all pairs are checked before the first one moves."""
     _need_cuda()
     if parent.dim() != 2 or parent.dtype != torch.int32 or not parent.is_contiguous():
         raise ValueError("parent: contiguous int32 [B, W]")
@@ -704,15 +706,21 @@ def q4_beam_reorder(pairs: Sequence, parent: torch.Tensor, dim: int = 0):
         raise ValueError("dim: not negative")
     B, W = parent.shape
     dev = _on_device(parent)
-    for first in range(0, len(pairs), REORDER_MAX):
-        group = pairs[first:first + REORDER_MAX]
-        fields = ()
-        for src, dst in group:
-            if src.get_device() != dev or dst.get_device() != dev:
-                raise ValueError("tensors must be on the current CUDA device")
-            fields += _reorder_item(src, dst, dim, B, W)
-        items = _REORDER_ARRAYS[len(group)](*fields)
-        _chk(lib().q4_beam_reorder(items, len(group), parent.data_ptr(), B, W, torch._C._cuda_getCurrentRawStream(dev)),
+    fields = ()
+    for src, dst in pairs:
+        if src.get_device() != dev or dst.get_device() != dev:
+            raise ValueError("tensors must be on the current CUDA device")
+        fields += _reorder_item(src, dst, dim, B, W)
+    n, stream = len(pairs), torch._C._cuda_getCurrentRawStream(dev)
+    if n == 0:
+        return
+    if n <= REORDER_MAX:
+        _chk(lib().q4_beam_reorder(_REORDER_ARRAYS[n](*fields), n, parent.data_ptr(), B, W, stream), "q4_beam_reorder")
+        return
+    items = (C.c_int64 * len(fields))(*fields)
+    _chk(lib().q4_beam_reorder_check(items, n, B, W), "q4_beam_reorder")
+    for first in range(0, n, REORDER_MAX):
+        _chk(lib().q4_beam_reorder(C.addressof(items) + first * C.sizeof(ReorderS), min(n - first, REORDER_MAX), parent.data_ptr(), B, W, stream),
              "q4_beam_reorder")
 
 

@@ -1998,30 +1998,59 @@ static bool reorder_extent(const void* base, const q4_reorder& t, int64_t row_st
   return true;
 }
 
-int q4_beam_reorder(const q4_reorder* items, int32_t n_items, const int32_t* parent, int32_t B, int32_t W, q4_stream stream) {
-  if (n_items < 0 || n_items > Q4_REORDER_MAX || B < 0 || W <= 0 || (int64_t)B * W > INT32_MAX) return Q4_ERR_DIM;
-  if (n_items == 0 || B == 0) return Q4_OK;
-  if (!items || !parent) return Q4_ERR_NULL;
-  if (!aligned_to(parent, 4)) return Q4_ERR_ALIGN;
-  const int64_t rows = (int64_t)B * W;
-  uint64_t lo[2][Q4_REORDER_MAX], hi[2][Q4_REORDER_MAX];   // src, dst
+// Checks of up to Q4_REORDER_MAX items by themselves, and the ranges of their rows ([0]: src, [1]: dst; empty where nothing is moved).
+struct ReorderRanges {
+  uint64_t lo[2][Q4_REORDER_MAX], hi[2][Q4_REORDER_MAX];
+};
+static int reorder_ranges(const q4_reorder* items, int n_items, int64_t rows, ReorderRanges& r) {
   for (int i = 0; i < n_items; ++i) {
     const q4_reorder& t = items[i];
     if (t.row_bytes < 0 || t.n[0] < 0 || t.n[1] < 0 || t.src_row_step < 0 || t.dst_row_step < 0) return Q4_ERR_DIM;
-    lo[0][i] = hi[0][i] = lo[1][i] = hi[1][i] = 0;
+    r.lo[0][i] = r.hi[0][i] = r.lo[1][i] = r.hi[1][i] = 0;
     if (t.row_bytes == 0 || t.n[0] == 0 || t.n[1] == 0) continue;
     if (!t.src || !t.dst) return Q4_ERR_NULL;
     if (rows > 1 && t.dst_row_step < t.row_bytes) return Q4_ERR_DIM;
     for (int d = 0; d < 2; ++d)
       if (t.src_step[d] < 0 || t.dst_step[d] < 0 || (t.n[d] > 1 && t.dst_step[d] < t.row_bytes)) return Q4_ERR_DIM;
     if ((__int128)t.n[0] * t.n[1] > ((int64_t)1 << 47) / rows) return Q4_ERR_DIM;   // (rows of dst lie apart)
-    if (!reorder_extent(t.src, t, t.src_row_step, t.src_step, rows, &lo[0][i], &hi[0][i]) ||
-        !reorder_extent(t.dst, t, t.dst_row_step, t.dst_step, rows, &lo[1][i], &hi[1][i]))
+    if (!reorder_extent(t.src, t, t.src_row_step, t.src_step, rows, &r.lo[0][i], &r.hi[0][i]) ||
+        !reorder_extent(t.dst, t, t.dst_row_step, t.dst_step, rows, &r.lo[1][i], &r.hi[1][i]))
       return Q4_ERR_DIM;
   }
-  for (int i = 0; i < n_items; ++i)
-    for (int j = 0; j < n_items; ++j)
-      if (lo[1][i] < hi[0][j] && lo[0][j] < hi[1][i]) return Q4_ERR_UNSUPPORTED;
+  return Q4_OK;
+}
+static int reorder_overlap(const ReorderRanges& dst, int n_dst, const ReorderRanges& src, int n_src) {
+  for (int i = 0; i < n_dst; ++i)
+    for (int j = 0; j < n_src; ++j)
+      if (dst.lo[1][i] < src.hi[0][j] && src.lo[0][j] < dst.hi[1][i]) return Q4_ERR_UNSUPPORTED;
+  return Q4_OK;
+}
+
+int q4_beam_reorder_check(const q4_reorder* items, int32_t n_items, int32_t B, int32_t W) {
+  if (n_items < 0 || B < 0 || W <= 0 || (int64_t)B * W > INT32_MAX) return Q4_ERR_DIM;
+  if (n_items == 0 || B == 0) return Q4_OK;
+  if (!items) return Q4_ERR_NULL;
+  const int64_t rows = (int64_t)B * W;
+  auto most = [&](int first) { return n_items - first < Q4_REORDER_MAX ? n_items - first : Q4_REORDER_MAX; };
+  for (int64_t i = 0; i < n_items; i += Q4_REORDER_MAX) {
+    ReorderRanges dst, src;
+    Q4_CHECK(reorder_ranges(items + i, most((int)i), rows, dst));
+    for (int64_t j = 0; j < n_items; j += Q4_REORDER_MAX) {
+      Q4_CHECK(reorder_ranges(items + j, most((int)j), rows, src));
+      Q4_CHECK(reorder_overlap(dst, most((int)i), src, most((int)j)));
+    }
+  }
+  return Q4_OK;
+}
+
+int q4_beam_reorder(const q4_reorder* items, int32_t n_items, const int32_t* parent, int32_t B, int32_t W, q4_stream stream) {
+  if (n_items < 0 || n_items > Q4_REORDER_MAX || B < 0 || W <= 0 || (int64_t)B * W > INT32_MAX) return Q4_ERR_DIM;
+  if (n_items == 0 || B == 0) return Q4_OK;
+  if (!items || !parent) return Q4_ERR_NULL;
+  if (!aligned_to(parent, 4)) return Q4_ERR_ALIGN;
+  ReorderRanges r;
+  Q4_CHECK(reorder_ranges(items, n_items, (int64_t)B * W, r));
+  Q4_CHECK(reorder_overlap(r, n_items, r, n_items));
   TagScope tag(TAG_REORDER);
   Q4_TRY(launch_beam_reorder(items, n_items, parent, B, W, S(stream)));
   return Q4_OK;

@@ -157,3 +157,39 @@ def test_select_of_equal_rows_and_of_nearly_equal_ones(Bd, dtype):
         assert len(set(got[:n].tolist())) == 1 and (len(set(got[n:].tolist())) == 1)
         want = -torch.logsumexp(z[0].double(), 1)[order]
         assert (got.double() - want).abs().max() < 1.3e-6 and got[n - 1] > got[n]
+
+
+# ---------------------------------------------------------------------------------------------------------- reorder
+def test_reorder_of_more_tensors_than_a_launch_is_checked_before_any_moves(Bd):
+    B, W = 2, 4
+    parent = torch.tensor([[1, 0, 3, 2], [2, 2, -1, 0]], dtype=torch.int32, device="cuda")
+    fresh = lambda n: [(torch.randn(B, W, 24, device="cuda"), torch.zeros(B, W, 24, device="cuda")) for _ in range(n)]
+    n = Bd.launch_count()
+    # the 17th (and the last of 40) reads what the first one writes
+    for count, at in ((17, 16), (40, 39), (40, 20)):
+        pairs = fresh(count)
+        pairs[at] = (pairs[0][1], pairs[at][1])
+        with pytest.raises(Bd.Q4Error) as err:
+            Bd.q4_beam_reorder(pairs, parent)
+        assert err.value.code == -6 and all((d == 0).all() for _, d in pairs)
+        pairs = fresh(count)
+        pairs[0] = (pairs[at][1][:, :, :], pairs[0][1])       # and the other way round
+        with pytest.raises(Bd.Q4Error) as err:
+            Bd.q4_beam_reorder(pairs, parent)
+        assert err.value.code == -6 and all((d == 0).all() for _, d in pairs)
+    # a 17th that is refused by its shape, its type, its device or in place
+    for bad in ((torch.zeros(B, W, 3, device="cuda"), torch.zeros(B, W, 4, device="cuda")),
+                (torch.zeros(B, W, 3, device="cuda"), torch.zeros(B, W, 3, device="cuda", dtype=torch.int32)),
+                (torch.zeros(B, W, 3), torch.zeros(B, W, 3)), (torch.zeros(W, B, 3, device="cuda"),) * 2, (fresh(1)[0][0],) * 2):
+        pairs = fresh(16) + [bad]
+        with pytest.raises((ValueError, Bd.Q4Error)):
+            Bd.q4_beam_reorder(pairs, parent)
+        assert all((d == 0).all() for _, d in pairs[:16])
+    assert Bd.launch_count() == n
+    pairs = fresh(40)
+    Bd.q4_beam_reorder(pairs, parent)
+    assert Bd.launch_count() == n + 3
+    for s, d in pairs:
+        for b in range(B):
+            for w, p in enumerate(parent[b].tolist()):
+                assert torch.equal(d[b, w], s[b, p] if p >= 0 else torch.zeros_like(d[b, w]))
