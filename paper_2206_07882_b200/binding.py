@@ -611,22 +611,29 @@ def q4_linear_token_scales(xq: torch.Tensor, x_scale: torch.Tensor, lin: DeviceL
     return out
 
 
-# Counters and workspaces of beam selections, one pair per device and stream: calls on one stream are ordered.  A capture gets
-# its own from the graph's memory.
+# Counters and workspaces of beam selections, one pair per device and stream: calls on one stream are ordered.  Each grows by itself to
+# the most that a call has asked for.  A capture gets its own from the graph's memory.
 _select_scratch: dict = {}
 
 
 def _scratch_of_select(like: torch.Tensor, dev: int, stream: int, counters: int, need: int) -> tuple:
-    entry = _select_scratch.get((dev, stream))
     capturing = _capturing()
-    if capturing or entry is None or entry[0].shape[0] < counters or entry[1].shape[0] < need:
-        new = like.new_zeros((max(counters, 1024),), dtype=torch.int32), like.new_empty((need,), dtype=torch.uint8)
-        if capturing:
-            return new
-        if entry is None and len(_select_scratch) >= _SCRATCH_STREAMS:
+    arrived = workspace = None
+    if not capturing:
+        entry = _select_scratch.get((dev, stream))
+        if entry is not None:
+            arrived, workspace = entry
+            if arrived.shape[0] >= counters and workspace.shape[0] >= need:
+                return entry
+        elif len(_select_scratch) >= _SCRATCH_STREAMS:
             del _select_scratch[next(iter(_select_scratch))]
-        entry = _select_scratch[dev, stream] = new
-    return entry
+    if arrived is None or arrived.shape[0] < counters:
+        arrived = like.new_zeros((max(counters, 1024),), dtype=torch.int32)
+    if workspace is None or workspace.shape[0] < need:
+        workspace = like.new_empty((need,), dtype=torch.uint8)
+    if not capturing:
+        _select_scratch[dev, stream] = arrived, workspace
+    return arrived, workspace
 
 
 def q4_lm_beam_select(logits: torch.Tensor, score: torch.Tensor, done: Optional[torch.Tensor] = None, eos: int = -1,
@@ -649,7 +656,8 @@ def q4_lm_beam_select(logits: torch.Tensor, score: torch.Tensor, done: Optional[
     if (s[2] != 1 and V > 1) or (B * W > 1 and ld < V) or (B > 1 and s[0] != W * ld):
         raise ValueError("logits: contiguous rows at one distance, beams within utterances")
     stream = torch._C._cuda_getCurrentRawStream(dev)
-    arrived, scratch = _scratch_of_select(score, dev, stream, B * (W + 1), _workspace_bytes(WS_LM_SELECT, (B, W, V)))
+    need = _workspace_bytes(WS_LM_SELECT, (B, W, V)) if workspace is None else 0
+    arrived, scratch = _scratch_of_select(score, dev, stream, B * (W + 1), need)
     if workspace is None:
         workspace = scratch
     parent, token, out = score.new_empty((3, B, W), dtype=torch.int32).unbind(0)

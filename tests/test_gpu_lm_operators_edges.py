@@ -193,3 +193,37 @@ def test_reorder_of_more_tensors_than_a_launch_is_checked_before_any_moves(Bd):
         for b in range(B):
             for w, p in enumerate(parent[b].tolist()):
                 assert torch.equal(d[b, w], s[b, p] if p >= 0 else torch.zeros_like(d[b, w]))
+
+
+# ------------------------------------------------------------------------------------------------- buffers of a call
+def test_select_keeps_its_buffers_where_shapes_alternate(Bd):
+    # many counters and little workspace, then the other way round: after one of each nothing is allocated any more
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        a = torch.randn(64, 16, 64, device="cuda"), torch.randn(64, 16, device="cuda")
+        b = torch.randn(1, 32, 400000, device="cuda"), torch.randn(1, 32, device="cuda")
+        want = [Bd.q4_lm_beam_select(*s) for s in (a, b)]
+        key = next(k for k in Bd._select_scratch if k[1] == stream.cuda_stream)
+        kept = [t.data_ptr() for t in Bd._select_scratch[key]]
+        n = Bd._select_scratch[key][1].numel()
+        assert n >= Bd.workspace_bytes(Bd.WS_LM_SELECT, b[0].shape) and Bd._select_scratch[key][0].numel() >= 64 * 17
+        for _ in range(3):
+            for s, w in zip((a, b), want):
+                got = Bd.q4_lm_beam_select(*s)
+                assert all(torch.equal(got[k], w[k]) for k in w)
+                assert [t.data_ptr() for t in Bd._select_scratch[key]] == kept
+    stream.synchronize()
+
+
+def test_select_with_the_callers_workspace_keeps_none_of_its_own(Bd):
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        z, score = torch.randn(1, 32, 400000, device="cuda"), torch.randn(1, 32, device="cuda")
+        need = Bd.workspace_bytes(Bd.WS_LM_SELECT, z.shape)
+        ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+        got = Bd.q4_lm_beam_select(z, score, workspace=ws)
+        held = sum(t.numel() * t.element_size() for k, e in Bd._select_scratch.items() if k[1] == stream.cuda_stream for t in e)
+        assert held < need                                    # counters alone
+        want = Bd.q4_lm_beam_select(z, score)
+        assert all(torch.equal(got[k], want[k]) for k in want)
+    stream.synchronize()
