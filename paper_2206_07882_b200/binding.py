@@ -368,6 +368,7 @@ class DeviceLinear:
         self.w, self.bias = w, bias
         self.prepared = None
         self.ws = None            # the workspace of the last call (its first word is the call's status)
+        self.status = torch.zeros(1, dtype=torch.int32, device=w.q.device)   # of q4_linear_token_scales, where a call brings none
         self.stream_ws = {}
 
     @staticmethod
@@ -585,7 +586,8 @@ def q4_linear_token_scales(xq: torch.Tensor, x_scale: torch.Tensor, lin: DeviceL
                            out_dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None,
                            status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Codes [M, k_pad] with one scale per row times 8-bit weights -> [M, rows of the weights] of out_dtype (or `out`, whose
-    rows may lie further apart).  `status`: one int32, zero before the first call (q4_poll_status)."""
+    rows may lie further apart).  `status`: one int32, zero before the first call, which receives an error where a bounded device wait
+    runs out and the output is not written (q4_poll_status); `lin.status` where none is given."""
     _need_cuda()
     w = lin.w
     dev = _on_device(xq, x_scale, w.q, out, status)
@@ -603,7 +605,9 @@ def q4_linear_token_scales(xq: torch.Tensor, x_scale: torch.Tensor, lin: DeviceL
         if out_dtype not in DTYPES or out.dim() != 2:
             raise ValueError("out: [M, rows of the weights] of fp32, fp16 or bf16")
         ld = _rows(out, M, w.rows, "out")
-    if status is not None and (status.dtype != torch.int32 or status.numel() < 1):
+    if status is None:
+        status = getattr(lin, "status", None)
+    elif status.dtype != torch.int32 or status.numel() < 1:
         raise ValueError("status: one int32")
     _chk(lib().q4_linear_token_scales(xq.data_ptr(), x_scale.data_ptr(), M, w.c(), _ptr(lin.bias), out.data_ptr(),
                                       DTYPES[out_dtype], ld, _ptr(status), torch._C._cuda_getCurrentRawStream(dev)),

@@ -1,4 +1,5 @@
 """The operators around a language model's output where a first set of tests did not look."""
+import ctypes as C
 from fractions import Fraction
 
 import numpy as np
@@ -227,3 +228,25 @@ def test_select_with_the_callers_workspace_keeps_none_of_its_own(Bd):
         want = Bd.q4_lm_beam_select(z, score)
         assert all(torch.equal(got[k], want[k]) for k in want)
     stream.synchronize()
+
+
+# ----------------------------------------------------------------------------------------------------------- linear
+@pytest.mark.parametrize("M,N,K", [(5, 300, 256), (16, 256, 4096), (1024, 4096, 256)])
+def test_linear_tells_of_a_wait_that_ran_out_without_being_asked(Bd, M, N, K):
+    # a layer has a status word of its own, which a call without one uses
+    w = torch.randint(-127, 128, (N, K), dtype=torch.int8, device="cuda").view(torch.uint8)
+    lin = Bd.DeviceLinear.from_mat(Bd.DeviceMat(w, torch.rand(N, device="cuda"), N, K, K, 8))
+    xq, sx = torch.randint(0, 255, (M, K), dtype=torch.uint8, device="cuda"), torch.rand(M, device="cuda")
+    want = Bd.q4_linear_token_scales(xq, sx, lin)
+    assert Bd.q4_poll_status(lin.status) == 0
+    assert Bd.lib().q4_test_wait_expiry_set(C.c_int32(1), C.c_uint32(1 << 12)) == 0
+    try:
+        Bd.q4_linear_token_scales(xq, sx, lin)
+        assert Bd.q4_poll_status(lin.status) == -8
+        own = torch.zeros(1, dtype=torch.int32, device="cuda")
+        lin.status.zero_()
+        Bd.q4_linear_token_scales(xq, sx, lin, status=own)
+        assert Bd.q4_poll_status(own) == -8 and Bd.q4_poll_status(lin.status) == 0
+    finally:
+        Bd.lib().q4_test_wait_expiry_set(C.c_int32(0), C.c_uint32(0))
+    assert torch.equal(Bd.q4_linear_token_scales(xq, sx, lin), want) and Bd.q4_poll_status(lin.status) == 0
