@@ -250,3 +250,23 @@ def test_linear_tells_of_a_wait_that_ran_out_without_being_asked(Bd, M, N, K):
     finally:
         Bd.lib().q4_test_wait_expiry_set(C.c_int32(0), C.c_uint32(0))
     assert torch.equal(Bd.q4_linear_token_scales(xq, sx, lin), want) and Bd.q4_poll_status(lin.status) == 0
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 40, 64), (33, 257, 640), (300, 1001, 1283)])
+@pytest.mark.parametrize("x_dtype", [torch.float32, torch.float16])
+def test_linear_of_the_frameworks_own_activations_and_weights(Bd, M, N, K, x_dtype):
+    # codes of quantize_pack_int4 with one MAX boundary a row, weights of DeviceMat.from_float_max
+    g = gen(M + N)
+    x, w = torch.randn(M, K, generator=g).to(x_dtype), torch.randn(N, K, generator=g)
+    x[M // 2] = 0                                             # (its boundary is 1)
+    lin = Bd.DeviceLinear.from_mat(Bd.DeviceMat.from_float_max(w.numpy(), 8), torch.randn(N, generator=g).cuda())
+    xq, sx = Bd.quantize_pack_int4(x.cuda(), Bd.Act(1.0, 1.0, 0, 8, 1), mode=1, n_groups=M, k_pad=lin.w.k_pad)
+    got = Bd.q4_linear_token_scales(xq, sx, lin).cpu().double()
+    values = lambda q, s: q.cpu().view(torch.int8).double() * s.cpu().double()[:, None]
+    acc = values(xq, sx) @ values(lin.w.q, lin.w.scale).t()
+    want = acc + lin.bias.cpu().double()
+    assert ((got - want).abs() <= (3 * 2.0 ** -24 * acc.abs() + 2.0 ** -23 * want.abs()) * 1.01 + 1e-38).all()
+    # and both are the real product to what 8 bits leave: half a step an operand and element, and what the rounded scales add
+    steps = (sx.cpu().double() / 2 * 1.01)[:, None] * w.double().abs().sum(1) + \
+        (lin.w.scale.cpu().double() / 2 * 1.01) * (x.double().abs() + sx.cpu().double()[:, None]).sum(1)[:, None]
+    assert ((got - lin.bias.cpu().double() - x.double() @ w.double().t()).abs() <= steps).all()
