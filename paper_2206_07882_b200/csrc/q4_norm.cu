@@ -185,7 +185,8 @@ __device__ __forceinline__ int exact_code(double v, double top) {
 }
 
 // A row in double, from memory: for rows that hold no more than zeros, a NaN or infinity, or values whose squares or products leave
-// the range of fp32, and for rows too long for registers.  Elements vec, vec + THREADS, ... of N are thread `t`'s, as everywhere.
+// the range of fp32, and for rows too long for registers.  Elements vec, vec + THREADS, ... of N are thread `t`'s, as everywhere; they are
+// counted without a sign, as the step behind the last one of a row of nearly 2^31 passes that.
 template <typename T, int THREADS>
 __device__ __noinline__ void norm_row(const NormArgs& a, long long row, int t, double (*s)[2]) {
   constexpr int N = Vec<T>::N;
@@ -194,8 +195,9 @@ __device__ __noinline__ void norm_row(const NormArgs& a, long long row, int t, d
   __syncwarp();   // (a neighbour may have stored part of a vector of the sum; wider groups have met at a barrier since)
   double sum = 0.0, top = 0.0;
   bool bad = false;
-  for (int v = t; v * N < a.k; v += THREADS)
-    for (int i = v * N; i < min(v * N + N, a.k); ++i) {
+  const uint32_t k = a.k, k_pad = a.k_pad;
+  for (uint32_t v = t; v * N < k; v += THREADS)
+    for (uint32_t i = v * N; i < min(v * N + N, k); ++i) {
       const double f = to_f32<T>(h[i]), p = fabs(f * (double)a.gain[i]);
       sum += f * f;
       top = fmax(top, p);
@@ -203,11 +205,11 @@ __device__ __noinline__ void norm_row(const NormArgs& a, long long row, int t, d
     }
   bad = row_any<THREADS>(bad);
   row_reduce<THREADS>(sum, top, s);
-  for (int v = t; v * N < a.k_pad; v += THREADS) {
+  for (uint32_t v = t; v * N < k_pad; v += THREADS) {
     int c[N];
     for (int i = 0; i < N; ++i) {
-      const int at = v * N + i;
-      c[i] = at < a.k && !bad && top > 0.0 ? exact_code((double)to_f32<T>(h[at]) * (double)a.gain[at], top) : 0;
+      const uint32_t at = v * N + i;
+      c[i] = at < k && !bad && top > 0.0 ? exact_code((double)to_f32<T>(h[at]) * (double)a.gain[at], top) : 0;
     }
     store_codes<N>(q + v * N, c);
   }
@@ -403,8 +405,9 @@ __global__ void __launch_bounds__(512) k_rmsnorm_quantize_long(const __grid_cons
       constexpr int N = Vec<T>::N;
       const T *x = static_cast<const T*>(a.x) + row * a.x_ld, *r = static_cast<const T*>(a.residual) + row * a.r_ld;
       T* out = static_cast<T*>(a.sum) + row * a.s_ld;
-      for (int v = threadIdx.x; v * N < a.k; v += 512)
-        for (int i = v * N; i < min(v * N + N, a.k); ++i) out[i] = from_f32<T>(__fadd_rn(to_f32<T>(x[i]), to_f32<T>(r[i])));
+      const uint32_t k = a.k;
+      for (uint32_t v = threadIdx.x; v * N < k; v += 512)
+        for (uint32_t i = v * N; i < min(v * N + N, k); ++i) out[i] = from_f32<T>(__fadd_rn(to_f32<T>(x[i]), to_f32<T>(r[i])));
     }
     norm_row<T, 512>(a, row, threadIdx.x, s_part64);
   }

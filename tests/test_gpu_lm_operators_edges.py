@@ -270,3 +270,18 @@ def test_linear_of_the_frameworks_own_activations_and_weights(Bd, M, N, K, x_dty
     steps = (sx.cpu().double() / 2 * 1.01)[:, None] * w.double().abs().sum(1) + \
         (lin.w.scale.cpu().double() / 2 * 1.01) * (x.double().abs() + sx.cpu().double()[:, None]).sum(1)[:, None]
     assert ((got - lin.bias.cpu().double() - x.double() @ w.double().t()).abs() <= steps).all()
+
+
+# -------------------------------------------------------------------------------------------------- rows of nearly 2^31
+@pytest.mark.parametrize("with_residual", [False, True])
+def test_norm_of_the_longest_row(Bd, with_residual):
+    k = 2 ** 31 - 32
+    x = torch.ones((1, k), dtype=torch.float16, device="cuda")
+    x[0, 0], x[0, -1] = 0.0, -2.0                             # 127 / 2 is a half: 64
+    residual = torch.zeros_like(x) if with_residual else None
+    codes, scale = Bd.q4_rmsnorm_quantize(x, torch.ones(k, device="cuda"), 1e-5, residual=residual, sum_out=residual)
+    codes = codes.view(torch.int8)
+    assert codes.shape == (1, k) and codes[0, 0].item() == 0 and codes[0, -1].item() == -127 and bool((codes[0, 1:-1] == 64).all())
+    want = 2 / np.sqrt((k + 2) / k + 1e-5) / 127
+    assert abs(scale.item() - want) <= 2.0 ** -24 * want * 1.01
+    assert residual is None or torch.equal(residual, x)
