@@ -221,14 +221,14 @@ __device__ __forceinline__ bool rank_candidates(const SelectShared& sh, int n, i
   }
   return true;
 }
-// The same by W passes over get(from) .. get(to - 1)
+// The same by W passes over get(from) .. get(to - 1) (counted without a sign: the step behind the last of nearly 2^31 passes that)
 template <typename F>
-__device__ __forceinline__ void best_by_passes(SelectShared& sh, F get, int from, int to, int W, Best* best) {
+__device__ __forceinline__ void best_by_passes(SelectShared& sh, F get, uint32_t from, uint32_t to, int W, Best* best) {
   const int tid = threadIdx.x;
   Best last{INFINITY, -1};
   for (int i = 0; i < W; ++i) {
     Best b{-INFINITY, INT32_MAX};
-    for (int k = from + tid; k < to; k += ROW_NT) {
+    for (uint32_t k = from + tid; k < to; k += ROW_NT) {
       const Best c = get(k);
       if (c.value > -INFINITY && before(last.value, last.label, c.value, c.label) && before(c.value, c.label, b.value, b.label)) b = c;
     }
@@ -378,10 +378,10 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
   }
   const bool far = top > -INFINITY && fabsf(top) > 1e6f;
   double total = sum * (double)pow2_down(scale - most);
-  const int from = part == 0 ? 0 : head + v0 * N, to = part + 1 == p.parts ? a.V : head + v1 * N;
+  const uint32_t from = part == 0 ? 0 : head + v0 * N, to = part + 1 == p.parts ? a.V : head + v1 * N;
   if (far) {   // differences from the maximum, which are exact where they count
     total = 0.0;
-    for (int k = from + tid; k < to; k += ROW_NT) total += (double)exp2_unit((to_f32<T>(z[k]) - top) * LOG2E);
+    for (uint32_t k = from + tid; k < to; k += ROW_NT) total += (double)exp2_unit((to_f32<T>(z[k]) - top) * LOG2E);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
@@ -398,7 +398,7 @@ __device__ __forceinline__ void best_of_segment(const LmSelectArgs& a, const Row
   }
   Best* best = p.best + out * W;
   if (noted > ROW_NOTED || !rank_candidates(sh, n, W, best))
-    best_by_passes(sh, [&](int k) { return Best{to_f32<T>(z[k]), k}; }, from, to, W, best);
+    best_by_passes(sh, [&](uint32_t k) { return Best{to_f32<T>(z[k]), (int32_t)k}; }, from, to, W, best);
 }
 
 // A row's segments put together in the place of the first one: the sum of their shares of the log-sum-exp, and the W best of their
@@ -456,7 +456,7 @@ __device__ __forceinline__ void merge_row(const RowParts& p, long long row, int 
     // many equal ones: best of passes into shared memory first, as it takes the place of what the passes read
     __syncthreads();
     Best* found = reinterpret_cast<Best*>(sh.row.value);
-    best_by_passes(sh, [&](int k) { return load_best(best + k); }, 0, entries, W, found);
+    best_by_passes(sh, [&](uint32_t k) { return load_best(best + k); }, 0, entries, W, found);
     __syncthreads();
     if (tid < W) best[tid] = found[tid];
   }

@@ -285,3 +285,17 @@ def test_norm_of_the_longest_row(Bd, with_residual):
     want = 2 / np.sqrt((k + 2) / k + 1e-5) / 127
     assert abs(scale.item() - want) <= 2.0 ** -24 * want * 1.01
     assert residual is None or torch.equal(residual, x)
+
+
+@pytest.mark.parametrize("level", [0.0, 2097152.0])          # (the latter is summed by differences from the maximum)
+def test_select_over_the_longest_row(Bd, level):
+    V = 2 ** 31 - 1
+    z = torch.full((1, 1, V), level, dtype=torch.bfloat16, device="cuda")
+    score = torch.zeros(1, 1, device="cuda")
+    tol = 5e-6 + 2.0 ** -24 * np.log(V) * 1.01
+    r = Bd.q4_lm_beam_select(z, score)                        # all alike: the first label
+    assert r["parent"].item() == 0 and r["token"].item() == 0 and abs(r["score"].item() + np.log(V)) <= tol
+    z[0, 0, 0], z[0, 0, V - 1] = -INF, level + 16384 if level else 8.0
+    r = Bd.q4_lm_beam_select(z, score)
+    want = 0.0 if level else 8 - np.log(V - 2 + np.exp(8.0))
+    assert r["token"].item() == V - 1 and abs(r["score"].item() - want) <= tol
