@@ -2,6 +2,7 @@
 import ctypes as C
 
 import pytest
+import torch
 
 P = C.c_void_p
 
@@ -53,3 +54,21 @@ def test_any_number_of_moves_is_checked_as_one_call(Bd):
         assert check(items) == 0
     assert check(fresh(2), n=-1) == -2 and check(fresh(2), W=0) == -2 and check(fresh(2), B=-1) == -2 and check(fresh(2), B=1 << 30) == -2
     assert check(fresh(2), B=0) == 0 and Bd.lib().q4_beam_reorder_check(None, 3, 2, 4) == -1
+
+
+def test_a_layer_over_weights_takes_only_what_its_sizes_say(Bd):
+    # (on the CPU: nothing is launched)
+    def mat(q=None, scale=None, rows=8, k=60, k_pad=64, bits=8):
+        return Bd.DeviceMat(torch.zeros(rows, k_pad * bits // 8, dtype=torch.uint8) if q is None else q,
+                            torch.ones(rows) if scale is None else scale, rows, k, k_pad, bits)
+    for bits in (2, 4, 8):
+        assert Bd.DeviceLinear.from_mat(mat(bits=bits), torch.zeros(8)).w.rows == 8
+    Bd.DeviceLinear.from_mat(mat(q=torch.zeros(8 * 64, dtype=torch.int8)))
+    for bad in (mat(q=torch.zeros(7, 64, dtype=torch.uint8)), mat(q=torch.zeros(8, 60, dtype=torch.uint8)), mat(q=torch.zeros(8, 64)),
+                mat(q=torch.zeros(64, 8, dtype=torch.uint8).t()), mat(scale=torch.ones(7)), mat(scale=torch.ones(8, 1)),
+                mat(scale=torch.ones(8, dtype=torch.float64)), mat(scale=torch.ones(16)[::2]), mat(scale=torch.ones(8, device="meta"))):
+        with pytest.raises(ValueError):
+            Bd.DeviceLinear.from_mat(bad)
+    for bias in (torch.zeros(7), torch.zeros(8, dtype=torch.float16), torch.zeros(16)[::2], torch.zeros(8, device="meta")):
+        with pytest.raises(ValueError):
+            Bd.DeviceLinear.from_mat(mat(), bias)
