@@ -432,7 +432,8 @@ int q4_feature_prologue(const float* mel, int32_t B, int32_t T100, int32_t M, vo
  * A row that holds a NaN or an infinity, or whose product with the gain does (a gain that is not finite does so to every row), gets
  * codes 0 and a NaN scale.  Values of any finite magnitude are accepted.
  *   x [rows, k] dtype, row stride x_stride; residual (nullable) and sum_out (required with residual, refused without)
- *   likewise; sum_out may be x or residual itself (same pointer and stride).  gain [k] fp32, 16-byte aligned.  0 <= eps, finite.
+ *   likewise; sum_out may be x or residual itself (same pointer and stride), else its rows lie apart from theirs.
+ *   gain [k] fp32, 16-byte aligned.  0 <= eps, finite.
  *   q_out [rows, k_pad] codes as for quantize_pack_int4 (k_pad a multiple of 32, elements behind k are 0); scale_out [rows].
  * Input of q4_linear_token_scales.  Counts as one activation quantizer (q4_quantizer_calls).
  */

@@ -264,8 +264,8 @@ __device__ __forceinline__ void pack(Vec<__nv_bfloat16>& v, const float (&f)[8])
 
 // A row per group of THREADS threads; everything is read and written once, the products v lie in registers, NV vectors of 16 bytes of
 // the row a thread.  WHOLE: rows are 16-byte aligned and a multiple of that long.
-// Long rows are bound by memory (4096 x 4096 with a residual: fp32 36.9 us, 5.9 TB/s; bf16 24.4 us, 4.8 TB/s), short ones of 16 bits
-// by their instructions, about 14 for each element, and waits that few warps cover (16000 x 1280 fp16 alone: 18.0 us, 3.4 TB/s; with a
+// Long rows are bound by memory (4096 x 4096 with a residual: fp32 36.9 us, 5.9 TB/s; bf16 24.5 us, 4.8 TB/s), short ones of 16 bits
+// by their instructions, about 14 for each element, and waits that few warps cover (16000 x 1280 fp16 alone: 17.7 us, 3.5 TB/s; with a
 // sixth vector that holds nothing 20.6; with the next row copied ahead to shared memory 22).  One warp a row needs no barrier;
 // wider groups take rows that a warp's registers do not hold, and few rows, where a row's latency is the call's (16 x 1024: 2.2 us).
 // Forming the products again for the codes, for registers of half as many bits, took 10 % more.  Rows that are not 16-byte

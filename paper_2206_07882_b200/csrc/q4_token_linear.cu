@@ -478,7 +478,8 @@ cudaError_t launch_pair(const TokenLinearArgs& a, cudaStream_t s) {
 
 // Time of a launch in us, fitted to all kernels' times at some 600 shapes (1 to 8192 tokens, 512 to 50257 channels, 640 to 14000
 // codes); the kernel with the least is taken, of equal ones that with more tokens a tile, which reads weights less often.  At those
-// shapes the choice takes 0.4 % longer than the fastest on average.  Examples, us for 32 / 64 tokens a tile / pairs of 128 / of 256:
+// shapes the choice takes 0.4 % longer than the fastest on average.  (Fitted by hand on one B200; another chip wants its own.)
+// Examples, us for 32 / 64 tokens a tile / pairs of 128 / of 256:
 // 64 x 4096 x 4096 7.8 / 8.3 / - / -, 300 x 5120 x 4096 19 / 13.1 / 10.9 / 15.5, 512 x 11000 x 8192 107 / 71 / 40 / 44.
 // A CTA alone: a tile's chunk of 128 codes takes as long as its operands need from the L2 (18 to 24 KB), the CTAs of an SM one after
 // the other, their epilogues behind the first, and all bytes at least their time in memory.  A split exchanges sums, 1 to 2.2 us
