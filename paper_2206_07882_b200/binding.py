@@ -375,9 +375,9 @@ class DeviceLinear:
     def from_mat(w: DeviceMat, bias: Optional[torch.Tensor] = None) -> "DeviceLinear":
         """A layer over weights that are on the device already (DeviceMat.from_float_max, for instance)."""
         lin = DeviceLinear.__new__(DeviceLinear)
-        _require(w.q.element_size() == 1 and w.q.is_contiguous() and w.q.numel() == w.rows * (w.k_pad * w.bits // 8),
+        _require(w.q.is_contiguous() and w.q.numel() * w.q.element_size() >= w.rows * (w.k_pad * w.bits // 8),
                  "w.q: contiguous codes, rows of k_pad")
-        _require(w.scale.dtype == torch.float32 and w.scale.shape == (w.rows,) and w.scale.is_contiguous() and w.scale.device == w.q.device,
+        _require(w.scale.dtype == torch.float32 and w.scale.numel() >= w.rows and w.scale.is_contiguous() and w.scale.device == w.q.device,
                  "w.scale: one contiguous fp32 value per weight row, beside the weights")
         _require(bias is None or (bias.dtype == torch.float32 and bias.shape == (w.rows,) and bias.is_contiguous()
                                   and bias.device == w.q.device), "bias: one contiguous fp32 value per weight row, beside the weights")

@@ -63,9 +63,10 @@ def test_a_layer_over_weights_takes_only_what_its_sizes_say(Bd):
                             torch.ones(rows) if scale is None else scale, rows, k, k_pad, bits)
     for bits in (2, 4, 8):
         assert Bd.DeviceLinear.from_mat(mat(bits=bits), torch.zeros(8)).w.rows == 8
-    Bd.DeviceLinear.from_mat(mat(q=torch.zeros(8 * 64, dtype=torch.int8)))
-    for bad in (mat(q=torch.zeros(7, 64, dtype=torch.uint8)), mat(q=torch.zeros(8, 60, dtype=torch.uint8)), mat(q=torch.zeros(8, 64)),
-                mat(q=torch.zeros(64, 8, dtype=torch.uint8).t()), mat(scale=torch.ones(7)), mat(scale=torch.ones(8, 1)),
+    for good in (mat(q=torch.zeros(8 * 64, dtype=torch.int8)), mat(q=torch.zeros(9, 64, dtype=torch.uint8), scale=torch.ones(8, 1))):
+        Bd.DeviceLinear.from_mat(good)
+    for bad in (mat(q=torch.zeros(7, 64, dtype=torch.uint8)), mat(q=torch.zeros(8, 60, dtype=torch.uint8)),
+                mat(q=torch.zeros(64, 8, dtype=torch.uint8).t()), mat(scale=torch.ones(7)),
                 mat(scale=torch.ones(8, dtype=torch.float64)), mat(scale=torch.ones(16)[::2]), mat(scale=torch.ones(8, device="meta"))):
         with pytest.raises(ValueError):
             Bd.DeviceLinear.from_mat(bad)
